@@ -89,7 +89,8 @@ typedef enum {
   E3_CALL_TOKEN_LOGP_ENTROPY = 1,
   E3_CALL_MASKED_MEAN_ENTROPY = 2,
   E3_CALL_GRPO_OBJECTIVE = 3,
-  E3_CALL_SEQUENCE_MEAN_ENTROPY = 4
+  E3_CALL_SEQUENCE_MEAN_ENTROPY = 4,
+  E3_CALL_VERIFY_DRAFTS = 5
 } e3_call;
 
 /* Human-readable name of a status code (static string). */
@@ -97,7 +98,8 @@ E3_API const char *e3_status_string(e3_status s);
 
 /* Bytes of device scratch a call uses for the given problem size.  For
  * E3_CALL_MASKED_MEAN_ENTROPY `rows` is the number of tokens n, for E3_CALL_GRPO_OBJECTIVE the number of
- * responses n_seq, for E3_CALL_SEQUENCE_MEAN_ENTROPY the number of sequences n_seq; V, dt are ignored for these.  E3_CALL_SAMPLE: 256 KiB for the partial states of cut rows plus
+ * responses n_seq, for E3_CALL_SEQUENCE_MEAN_ENTROPY the number of sequences n_seq, for E3_CALL_VERIFY_DRAFTS the number of
+ * logits rows n_seq * (max_draft + 1); V, dt are ignored for these.  E3_CALL_SAMPLE: 256 KiB for the partial states of cut rows plus
  * room for the sums of blocks (about 1/32 of the bytes of the logits), which the present kernels leave untouched;
  * E3_CALL_TOKEN_LOGP_ENTROPY: 256 KiB plus the partial sums of the fused mean entropy.
  * Scratch contents on entry never matter.  A workspace must not be shared by calls that can run
@@ -197,6 +199,88 @@ E3_API e3_status e3_token_logp_entropy_backward(const void *logits, e3_dtype dt,
                                          const float *temps, float temp_scalar, const float *logp, const float *ent,
                                          const float *g_logp, const float *g_ent, void *dlogits,
                                          int64_t dlogits_stride, void *stream);
+
+/*
+ * Rollout step with drafted tokens (speculative decoding): which drafts of every sequence are kept, and the token that follows them,
+ * so that the emitted tokens are distributed as if e3_sample had drawn each of them from the target.
+ *
+ * Sequence b has len_b = draft_len[b] drafts d_0, d_1, ... and the target's logits at the len_b + 1 positions that begin with
+ * them; p_j = softmax(logits / temps[b]) at position j.  The draft's distribution q_j is softmax(draft_logits / draft_temps[b]), its
+ * normaliser taken from draft_logp: ln q_j(i) = (y_i - y_d) / tau' + draft_logp; without draft_logits (tokens copied from the prompt),
+ * and where draft_temps[b] is 0, it is 1 at d_j and 0 elsewhere.  With a = the number of leading drafts with
+ *   u_j q_j(d_j) < p_j(d_j),
+ * the drafts before position a are kept, and one more token is drawn at position a: from r = max(p_a - q_a, 0) where a draft was refused
+ * (from p_a if nothing is left of r), from p_a behind the last draft.  The draw is that of E3_SAMPLER_BLOCK with the caller's uniforms: the block of
+ * E3_SAMPLE_BLOCK entries with the largest ln(sum r_i) - ln(-ln v_b), then the first entry of it whose prefix sum exceeds w times its
+ * sum; ties go to the lower index.  Comparisons that fp32 leaves open are made in fp64.
+ *
+ *   logits        device, [n_seq * (max_draft + 1), V] with row_stride elements from row to row, position j of sequence b in row
+ *                 b (max_draft + 1) + j; rows behind a sequence's last position are not read
+ *   temps         device float [n_seq]; 0 is greedy (p is 1 at the lowest-index arg-max)
+ *   draft_tok     device int32 [n_seq, max_draft]; a token outside [0, V), or one whose draft logit, draft_logp or draft temperature cannot
+ *                 be used, is refused and the draw is from p_a
+ *   draft_len     device int32 [n_seq] or NULL (= all max_draft); values outside [0, max_draft] are taken as the nearer end
+ *   draft_logits  device, type dt, [n_seq * max_draft, V] with draft_stride elements from row to row, or NULL
+ *   draft_temps   device float [n_seq] or NULL (= temps);  draft_logp: device float [n_seq, max_draft], e3_sample's out_logp on the draft's
+ *                 logits; both are used with draft_logits alone.  An entry whose draft logit is NaN or +inf is not drawn.
+ *   uniforms      device double, [n_seq, max_draft + ceil(V / E3_SAMPLE_BLOCK) + 1] with uniform_stride entries from row to row, in [0, 1): u_j, v_b, w
+ *   out_tok       device int32 [n_seq, max_draft + 1]: the kept drafts, the drawn token, then -1
+ *   out_kept      device int32 [n_seq]: a
+ *   out_logp, out_ent   device float [n_seq, max_draft + 1], each may be NULL: log-probability of the emitted token under p_j, entropy
+ *                 of p_j; 0 behind the drawn token
+ *   workspace     e3_workspace_bytes(E3_CALL_VERIFY_DRAFTS, n_seq * (max_draft + 1), 0, 0) bytes of device scratch
+ * A position that is reached and whose row holds NaN or +inf or nothing but -inf, whose temperature is negative or not finite, or whose
+ * uniform lies outside [0, 1) ends the sequence: token -1, log-probability and entropy NaN.  n_seq * (max_draft + 1) < 2^26.
+ */
+E3_API e3_status e3_verify_drafts(const void *logits, e3_dtype dt, int64_t n_seq, int64_t max_draft, int64_t V, int64_t row_stride,
+                                  const float *temps, const int32_t *draft_tok, const int32_t *draft_len,
+                                  const void *draft_logits, int64_t draft_stride, const float *draft_temps,
+                                  const float *draft_logp, const double *uniforms, int64_t uniform_stride, int32_t *out_tok,
+                                  int32_t *out_kept, float *out_logp, float *out_ent, void *workspace, size_t workspace_bytes,
+                                  void *stream);
+
+/*
+ * The vectors of tokens (a model's input embedding): out[t] = scale * table[tok[t]], rounded once to dt.
+ *
+ *   tok         device int32 [n]; -1 (padding, or a row that a sampling call marked) gives zeros, any other token outside
+ *               [0, V) a row of NaN
+ *   table       device, type dt, [V, D] with table_stride elements from row to row
+ *   out         device, type dt, [n, D] with out_stride elements from row to row; must not overlap table
+ * Tables and outputs whose rows all begin on a 16-byte boundary move in vectors.
+ */
+E3_API e3_status e3_embed_tokens(const int32_t *tok, int64_t n, const void *table, e3_dtype dt, int64_t V, int64_t D,
+                                 int64_t table_stride, float scale, void *out, int64_t out_stride, void *stream);
+
+/*
+ * Gradient of the table: dtable[v] = scale * sum over t with tok[t] == v of g[t], added in fp32 in a fixed order and rounded once
+ * (with accumulate != 0 dtable[v] += the same; rows of tokens that do not occur are then left alone, else they become 0).  Tokens
+ * outside [0, V) contribute nothing.  The tokens are sorted first; nothing depends on the order of atomic operations.
+ *
+ *   g           device, type dt, [n, D] with g_stride elements from row to row
+ *   dtable      device, type table_dt (it may be wider than dt), [V, D] with dtable_stride elements from row to row; must not overlap g
+ *   workspace   e3_embed_workspace_bytes(n, V, D) bytes of device scratch (0 for sizes that the call rejects, and for n == 0)
+ * n < 2^31, V <= 2^22, D < 2^24.
+ */
+E3_API size_t e3_embed_workspace_bytes(int64_t n, int64_t V, int64_t D);
+E3_API e3_status e3_embed_tokens_backward(const int32_t *tok, int64_t n, const void *g, e3_dtype dt, int64_t V, int64_t D,
+                                          int64_t g_stride, float scale, void *dtable, e3_dtype table_dt,
+                                          int64_t dtable_stride, int accumulate, void *workspace, size_t workspace_bytes,
+                                          void *stream);
+
+/*
+ * Values in 8 bits (e4m3) with one scale for each E3_SCALE_BLOCK columns of a row (block_rows == 1: hidden states) or for each
+ * E3_SCALE_BLOCK x E3_SCALE_BLOCK entries (block_rows == E3_SCALE_BLOCK: the vocabulary's table).  The scale of a block is the smallest power of
+ * two s (not below 2^-126; 1 for a block of zeros) with max |x| <= 448 s, so that x / s is exact; q = x / s rounded to nearest even.  A
+ * block that holds NaN or an infinity gets the scale NaN and values NaN.
+ *
+ *   x           device, type dt, [rows, cols] with row_stride elements from row to row
+ *   q           device bytes, [rows, cols] with q_stride bytes from row to row; what lies between two rows is left alone
+ *   scale       device float, [ceil(rows / block_rows), ceil(cols / E3_SCALE_BLOCK)] with scale_stride entries from row to row
+ * rows, cols < 2^31.
+ */
+#define E3_SCALE_BLOCK 128
+E3_API e3_status e3_quantize(const void *x, e3_dtype dt, int64_t rows, int64_t cols, int64_t row_stride, int32_t block_rows,
+                             uint8_t *q, int64_t q_stride, float *scale, int64_t scale_stride, void *stream);
 
 /*
  * Batch entropy H_t of the scheduler (Sec. 4.2: "average entropy" of a batch), read as the mean

@@ -22,13 +22,16 @@ E3_F32, E3_BF16 = 0, 1
 E3_SAMPLER_TOKEN, E3_SAMPLER_BLOCK, E3_SAMPLER_TOKEN_AUDIT = 0, 1, 2
 E3_CALL_SAMPLE, E3_CALL_TOKEN_LOGP_ENTROPY, E3_CALL_MASKED_MEAN_ENTROPY, E3_CALL_GRPO_OBJECTIVE = 0, 1, 2, 3
 E3_CALL_SEQUENCE_MEAN_ENTROPY = 4
+E3_CALL_VERIFY_DRAFTS = 5
 E3_SAMPLE_BLOCK = 256
+E3_SCALE_BLOCK = 128
 
 EXPORTS = ("e3_status_string", "e3_workspace_bytes", "e3_sample", "e3_token_logp_entropy",
            "e3_token_logp_entropy_backward", "e3_grpo_objective",
            "e3_masked_mean_entropy", "e3_masked_mean_entropy_static", "e3_group_advantage", "e3_allocate_budget", "e3_update_temperature",
            "e3_anneal_target", "e3_entropy_gap", "e3_update_temperature_gap", "e3_difficulty_accumulate", "e3_difficulty_rank", "e3_budget_curriculum",
-           "e3_test_arm_stall", "e3_test_row_blocks", "e3_probe_read", "e3_sequence_mean_entropy")
+           "e3_test_arm_stall", "e3_test_row_blocks", "e3_probe_read", "e3_sequence_mean_entropy",
+           "e3_verify_drafts", "e3_embed_tokens", "e3_embed_workspace_bytes", "e3_embed_tokens_backward", "e3_quantize")
 
 
 class E3Error(RuntimeError):
@@ -116,6 +119,22 @@ def lib() -> C.CDLL:
         L.e3_anneal_target.argtypes = [C.POINTER(e3_sched)]
         L.e3_probe_read.restype = C.c_int
         L.e3_probe_read.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.e3_verify_drafts.restype = C.c_int
+        L.e3_verify_drafts.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p,
+                                       C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
+                                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.e3_embed_tokens.restype = C.c_int
+        L.e3_embed_tokens.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_float,
+                                      C.c_void_p, C.c_int64, C.c_void_p]
+        L.e3_embed_workspace_bytes.restype = C.c_size_t
+        L.e3_embed_workspace_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int64]
+        L.e3_embed_tokens_backward.restype = C.c_int
+        L.e3_embed_tokens_backward.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64,
+                                               C.c_float, C.c_void_p, C.c_int, C.c_int64, C.c_int, C.c_void_p, C.c_size_t,
+                                               C.c_void_p]
+        L.e3_quantize.restype = C.c_int
+        L.e3_quantize.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int64,
+                                  C.c_void_p, C.c_int64, C.c_void_p]
         L.e3_test_row_blocks.restype = C.c_int32
         L.e3_test_row_blocks.argtypes = [C.c_int, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
         L.e3_test_arm_stall.restype = None
@@ -150,6 +169,10 @@ def _stream(stream) -> int:
     return s.cuda_stream
 
 
+def e3_embed_workspace_bytes(n: int, V: int, D: int) -> int:
+    return int(lib().e3_embed_workspace_bytes(n, V, D))
+
+
 def e3_workspace_bytes(which: int, rows: int, V: int = 0, dt: int = E3_F32) -> int:
     return int(lib().e3_workspace_bytes(which, rows, V, dt))
 
@@ -179,6 +202,45 @@ def e3_token_logp_entropy_backward(logits, targets, logp, ent, g_logp=None, g_en
                                    temp_scalar: float = 1.0, out=None, stream=None):
     """Gradient of the training-side outputs with respect to the logits: tensor like ``logits``."""
     return _nat.token_logp_entropy_backward(logits, targets, logp, ent, g_logp, g_ent, mask, temps, temp_scalar, out, stream)
+
+
+def e3_verify_drafts(logits, temps, draft_tok, uniforms, draft_len=None, draft_logits=None, draft_temps=None, draft_logp=None,
+                     out_tok=None, out_kept=None, out_logp=None, out_ent=None, want_logp: bool = True, want_ent: bool = True,
+                     workspace=None, stream=None):
+    """Rollout step with drafted tokens.  ``logits`` [n_seq * (K + 1), V], ``temps`` [n_seq], ``draft_tok`` int32 [n_seq, K], ``uniforms``
+    float64 [n_seq, K + ceil(V / 256) + 1] in [0, 1).  Returns (tok int32 [n_seq, K + 1], kept int32 [n_seq], logp float32 | None,
+    ent float32 | None, both [n_seq, K + 1]): the kept drafts, the token drawn behind them, then -1."""
+    return _nat.verify_drafts(logits, temps, draft_tok, uniforms, draft_len, draft_logits, draft_temps, draft_logp, out_tok, out_kept,
+                              out_logp, out_ent, want_logp, want_ent, workspace, stream)
+
+
+def e3_embed_tokens(table, tok, scale: float = 1.0, out=None, stream=None):
+    """``scale`` times the rows of ``table`` [V, D] that ``tok`` (int32, any shape) names: tensor [*tok.shape, D] like ``table``.  -1 gives
+    zeros, any other token outside [0, V) NaN.  ``out``: 2-D, one row per token."""
+    return _nat.embed_tokens(table, tok, scale, out, stream)
+
+
+_DTYPE_CODES = {None: -1, torch.float32: E3_F32, torch.bfloat16: E3_BF16}
+
+
+def _dtype_code(dtype) -> int:
+    code = _DTYPE_CODES.get(dtype)
+    if code is None:
+        raise ValueError("dtype must be torch.float32 or torch.bfloat16")
+    return code
+
+
+def e3_embed_tokens_backward(g, tok, V: int, scale: float = 1.0, out=None, accumulate: bool = False, dtype=None, workspace=None,
+                             stream=None):
+    """Gradient of the table of :func:`e3_embed_tokens`: tensor [V, D] of ``dtype`` (default: that of ``g`` [n, D]).  With ``accumulate`` the
+    gradient is added to ``out``, else ``out`` is overwritten."""
+    return _nat.embed_tokens_backward(g, tok, V, scale, out, accumulate, _dtype_code(dtype), workspace, stream)
+
+
+def e3_quantize(x, block_rows: int = 1, out_q=None, out_scale=None, stream=None):
+    """``x`` [rows, cols] in 8 bits with a scale per ``block_rows`` x 128 entries (1 for hidden states, 128 for the vocabulary's table).
+    Returns (q float8_e4m3fn [rows, cols], its rows 16-byte aligned, scale float32 [ceil(rows / block_rows), ceil(cols / 128)])."""
+    return _nat.quantize(x, block_rows, out_q, out_scale, stream)
 
 
 def e3_masked_mean_entropy(ent, mask=None, out=None, workspace=None, stream=None):

@@ -1,0 +1,609 @@
+// Embedding of tokens, out[t] = scale E[tok_t], and the gradient of its table, dE[v] = scale sum_{t: tok_t = v} g[t].
+//
+// The gradient adds in a fixed order and without atomics on floating-point values: the tokens are sorted (stable, by two digits: first by
+// the upper one across tiles of tokens, then every bucket by the lower one in one CTA), the sorted positions are cut into segments of equal
+// length, and a CTA adds the rows of g of a segment in 32 bits.  A token whose run lies within a segment is finished there; the others
+// leave a partial sum per segment, and a last kernel adds those in order.  Rows of tokens that do not occur are zeroed by CTAs of the
+// same launch that reads g, so that reads and writes share the memory.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math_constants.h>
+#include <stdint.h>
+
+#include "e3.h"
+
+namespace e3 {
+namespace {
+
+constexpr int kDigitsMost = 1024;    // buckets of the upper digit
+constexpr int kLowMost = 12;         // bits of the lower digit
+constexpr int kTilesMost = 512;
+constexpr int64_t kVMost = int64_t(kDigitsMost) << kLowMost;
+constexpr int64_t kDMost = int64_t(1) << 24;  // (columns are blockIdx.y)
+static_assert(kDMost / 256 <= 65536, "grid");
+
+template <int DT>
+struct Elem;
+template <>
+struct Elem<0> {
+  using T = float;
+  static constexpr int kVec = 4;
+  static __device__ __forceinline__ float get(T v) { return v; }
+  static __device__ __forceinline__ T put(float v) { return v; }
+};
+template <>
+struct Elem<1> {
+  using T = __nv_bfloat16;
+  static constexpr int kVec = 8;
+  static __device__ __forceinline__ float get(T v) { return __bfloat162float(v); }
+  static __device__ __forceinline__ T put(float v) { return __float2bfloat16_rn(v); }  // one rounding, to nearest even
+};
+
+// N consecutive elements (N = a 16-byte vector of them, or 1).
+template <int DT, int N>
+__device__ __forceinline__ void load_n(const typename Elem<DT>::T *p, float (&v)[N]) {
+  if constexpr (N == 1) {
+    v[0] = Elem<DT>::get(*p);
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; k += Elem<DT>::kVec) {
+      const uint4 w = *reinterpret_cast<const uint4 *>(p + k);
+      const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (DT == 0) {
+          v[k + i] = __uint_as_float(x[i]);
+        } else {
+          v[k + 2 * i] = __uint_as_float(x[i] << 16);
+          v[k + 2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
+        }
+      }
+    }
+  }
+}
+template <int DT, int N>
+__device__ __forceinline__ void store_n(typename Elem<DT>::T *p, const float (&v)[N]) {
+  if constexpr (N == 1) {
+    *p = Elem<DT>::put(v[0]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; k += Elem<DT>::kVec) {
+      uint32_t x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (DT == 0) {
+          x[i] = __float_as_uint(v[k + i]);
+        } else {
+          const __nv_bfloat162 h = __floats2bfloat162_rn(v[k + 2 * i], v[k + 2 * i + 1]);
+          x[i] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+      }
+      *reinterpret_cast<uint4 *>(p + k) = make_uint4(x[0], x[1], x[2], x[3]);
+    }
+  }
+}
+
+__device__ __forceinline__ void wait_for_stream_predecessor() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+// ---- lookup ------------------------------------------------------------------------------------------------------
+struct EmbedParams {
+  const int32_t *tok;
+  const void *table;
+  void *out;
+  int64_t n, V, D, table_stride, out_stride;
+  float scale;
+  int64_t segs;  // a row is cut into this many pieces of `len` vectors (a warp each)
+  int len;
+};
+
+constexpr int kEmbedWarps = 8;
+constexpr int kEmbedVecs = 4;  // vectors under way per lane
+
+// A warp takes a piece of a row: bound by the two moves of the row through memory; the token's number has to come first.
+template <int DT, int N>
+__global__ void __launch_bounds__(kEmbedWarps * 32) embed_kernel(const __grid_constant__ EmbedParams p) {
+  using E = Elem<DT>;
+  wait_for_stream_predecessor();
+  const int lane = threadIdx.x & 31;
+  const int64_t items = p.n * p.segs;
+  for (int64_t item = (int64_t)blockIdx.x * kEmbedWarps + (threadIdx.x >> 5); item < items; item += (int64_t)gridDim.x * kEmbedWarps) {
+    const int64_t t = item / p.segs, seg = item - t * p.segs;
+    const int64_t tok = p.tok[t];
+    const bool live = (uint64_t)tok < (uint64_t)p.V;
+    const float fill = tok == -1 ? 0.f : CUDART_NAN_F;
+    const int64_t c0 = seg * p.len * N, whole = p.D / N * N;
+    const int64_t c1 = c0 + (int64_t)p.len * N < whole ? c0 + (int64_t)p.len * N : whole;
+    const typename E::T *src = static_cast<const typename E::T *>(p.table) + (live ? tok : 0) * p.table_stride;
+    typename E::T *dst = static_cast<typename E::T *>(p.out) + t * p.out_stride;
+    for (int64_t c = c0 + lane * N; c < c1; c += 32 * N * kEmbedVecs) {
+      float v[kEmbedVecs][N];
+#pragma unroll
+      for (int k = 0; k < kEmbedVecs; ++k)
+        if (live && c + k * 32 * N < c1) load_n<DT, N>(src + c + k * 32 * N, v[k]);
+#pragma unroll
+      for (int k = 0; k < kEmbedVecs; ++k) {
+        if (c + k * 32 * N >= c1) break;
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[k][i] = live ? v[k][i] * p.scale : fill;
+        store_n<DT, N>(dst + c + k * 32 * N, v[k]);
+      }
+    }
+    // entries behind the last whole vector
+    if (N > 1 && seg == p.segs - 1 && whole + lane < p.D)
+      dst[whole + lane] = E::put(live ? E::get(src[whole + lane]) * p.scale : fill);
+  }
+}
+
+// ---- sorting -----------------------------------------------------------------------------------------------------
+struct SortParams {
+  const int32_t *tok;
+  int64_t n, V;
+  int low;               // bits of the lower digit
+  int digits;            // values of the upper one
+  int tiles;
+  int64_t tile;          // tokens of a tile
+  int32_t *counts;       // [tiles][digits]
+  uint2 *pairs;          // by the upper digit: (token, position)
+  int32_t *keys, *perm;  // sorted: tokens, positions
+  int32_t *start;        // [V + 1]: first sorted position of every token
+};
+
+constexpr int kCountThreads = 256;
+__global__ void __launch_bounds__(kCountThreads) count_kernel(const __grid_constant__ SortParams p) {
+  __shared__ int32_t hist[kDigitsMost];
+  for (int d = threadIdx.x; d < p.digits; d += kCountThreads) hist[d] = 0;
+  __syncthreads();
+  wait_for_stream_predecessor();
+  const int64_t lo = blockIdx.x * p.tile, hi = lo + p.tile < p.n ? lo + p.tile : p.n;
+  for (int64_t t = lo + threadIdx.x; t < hi; t += kCountThreads) {
+    const int64_t tok = p.tok[t];
+    if ((uint64_t)tok < (uint64_t)p.V) atomicAdd(&hist[tok >> p.low], 1);
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < p.digits; d += kCountThreads) p.counts[(int64_t)blockIdx.x * p.digits + d] = hist[d];
+}
+
+// Exclusive sums of x[0..n) in place, by a whole CTA; returns the total.  `sh`: 32 words.
+__device__ __forceinline__ int32_t scan_in_place(int32_t *x, int n, int32_t *sh) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  int32_t carry = 0;
+  for (int base = 0; base < n; base += (int)blockDim.x) {
+    const int i = base + (int)threadIdx.x;
+    const int32_t own = i < n ? x[i] : 0;
+    int32_t v = own;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int32_t up = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += up;
+    }
+    if (lane == 31) sh[warp] = v;
+    __syncthreads();
+    if (warp == 0) {
+      int32_t s = lane < warps ? sh[lane] : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int32_t up = __shfl_up_sync(0xffffffffu, s, o);
+        if (lane >= o) s += up;
+      }
+      sh[lane] = s;
+    }
+    __syncthreads();
+    if (i < n) x[i] = carry + v - own + (warp > 0 ? sh[warp - 1] : 0);
+    carry += sh[warps - 1];
+    __syncthreads();
+  }
+  return carry;
+}
+
+// Places of a warp's entries, 32 at a time and in their order: count[d] is the next place of digit d.
+__device__ __forceinline__ int32_t place_of(int32_t *count, int d, bool valid) {
+  const int lane = threadIdx.x & 31;
+  const uint32_t peers = __match_any_sync(0xffffffffu, valid ? d : -1);
+  const int before = __popc(peers & ((1u << lane) - 1u));
+  int32_t at = 0;
+  if (valid) at = count[d] + before;
+  __syncwarp();
+  if (valid && before == 0) count[d] += __popc(peers);
+  __syncwarp();
+  return at;
+}
+
+constexpr int kScatterWarps = 8;
+__global__ void __launch_bounds__(kScatterWarps * 32) scatter_kernel(const __grid_constant__ SortParams p) {
+  extern __shared__ int32_t dyn[];
+  __shared__ int32_t sh[32];
+  int32_t *const base = dyn;                // [digits]
+  int32_t *const hist = dyn + p.digits;     // [warps][digits]
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int d = threadIdx.x; d < p.digits * kScatterWarps; d += kScatterWarps * 32) hist[d] = 0;
+  wait_for_stream_predecessor();
+  __syncthreads();
+  // entries of every digit in this tile's predecessors, and in all tiles
+  for (int d = threadIdx.x; d < p.digits; d += kScatterWarps * 32) {
+    int32_t mine = 0, all = 0;
+#pragma unroll 8
+    for (int t = 0; t < p.tiles; ++t) {
+      const int32_t c = p.counts[(int64_t)t * p.digits + d];
+      if (t < (int)blockIdx.x) mine += c;
+      all += c;
+    }
+    base[d] = all;
+    hist[d] = mine;  // (kept in the first warp's row for a moment)
+  }
+  __syncthreads();
+  scan_in_place(base, p.digits, sh);
+  for (int d = threadIdx.x; d < p.digits; d += kScatterWarps * 32) {
+    base[d] += hist[d];
+    hist[d] = 0;
+  }
+  __syncthreads();
+  // the warps take consecutive parts of the tile
+  const int64_t part = p.tile / kScatterWarps;  // a multiple of 32
+  const int64_t lo = blockIdx.x * p.tile + warp * part, hi = lo + part < p.n ? lo + part : p.n;
+  int32_t *const own = hist + warp * p.digits;
+  for (int64_t t = lo + lane; t < hi; t += 32) {
+    const int64_t tok = p.tok[t];
+    if ((uint64_t)tok < (uint64_t)p.V) atomicAdd(&own[tok >> p.low], 1);
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < p.digits; d += kScatterWarps * 32) {
+    int32_t at = base[d];
+    for (int w = 0; w < kScatterWarps; ++w) {
+      const int32_t c = hist[w * p.digits + d];
+      hist[w * p.digits + d] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+  for (int64_t t0 = lo; t0 < hi; t0 += 32) {
+    const int64_t t = t0 + lane;
+    const int64_t tok = t < hi ? p.tok[t] : -1;
+    const bool valid = (uint64_t)tok < (uint64_t)p.V;
+    const int32_t at = place_of(own, (int)(tok >> p.low), valid);
+    if (valid) p.pairs[at] = make_uint2((uint32_t)tok, (uint32_t)t);
+  }
+}
+
+// One CTA sorts one bucket by the lower digit.
+__global__ void bucket_kernel(const __grid_constant__ SortParams p) {
+  extern __shared__ int32_t dyn[];
+  __shared__ int32_t sh[32];
+  __shared__ int32_t bounds[2];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, threads = blockDim.x;
+  const int bins = 1 << p.low, bucket = blockIdx.x;
+  int32_t *const total = dyn;          // [bins]
+  int32_t *const hist = dyn + bins;    // [warps][bins]
+  for (int d = threadIdx.x; d < bins * warps; d += threads) hist[d] = 0;
+  if (threadIdx.x < 2) bounds[threadIdx.x] = 0;
+  wait_for_stream_predecessor();
+  __syncthreads();
+  {  // entries before this bucket, and in it
+    int32_t before = 0, mine = 0;
+    for (int t = warp; t < p.tiles; t += warps) {
+#pragma unroll 4
+      for (int d = lane; d <= bucket; d += 32) {
+        const int32_t c = p.counts[(int64_t)t * p.digits + d];
+        if (d < bucket) before += c;
+        else mine += c;
+      }
+    }
+    before = __reduce_add_sync(0xffffffffu, before);
+    mine = __reduce_add_sync(0xffffffffu, mine);
+    if (lane == 0) {
+      atomicAdd(&bounds[0], before);
+      atomicAdd(&bounds[1], mine);
+    }
+  }
+  __syncthreads();
+  const int32_t first = bounds[0], count = bounds[1];
+  const uint2 *const pairs = p.pairs + first;
+  const int32_t part = ((count + warps - 1) / warps + 31) / 32 * 32;
+  const int32_t lo = warp * part < count ? warp * part : count, hi = lo + part < count ? lo + part : count;
+  int32_t *const own = hist + warp * bins;
+  for (int32_t i = lo + lane; i < hi; i += 32) atomicAdd(&own[pairs[i].x & (uint32_t)(bins - 1)], 1);
+  __syncthreads();
+  for (int d = threadIdx.x; d < bins; d += threads) {
+    int32_t s = 0;
+    for (int w = 0; w < warps; ++w) s += hist[w * bins + d];
+    total[d] = s;
+  }
+  __syncthreads();
+  scan_in_place(total, bins, sh);
+  for (int d = threadIdx.x; d < bins; d += threads) {
+    int32_t at = first + total[d];
+    const int64_t v = ((int64_t)bucket << p.low) + d;
+    if (v < p.V) p.start[v] = at;
+    for (int w = 0; w < warps; ++w) {
+      const int32_t c = hist[w * bins + d];
+      hist[w * bins + d] = at;
+      at += c;
+    }
+    if (v == p.V - 1) p.start[p.V] = at;
+  }
+  __syncthreads();
+  for (int32_t i0 = lo; i0 < hi; i0 += 32) {
+    const bool valid = i0 + lane < hi;
+    const uint2 e = valid ? pairs[i0 + lane] : make_uint2(0u, 0u);
+    const int32_t at = place_of(own, (int)(e.x & (uint32_t)(bins - 1)), valid);
+    if (valid) {
+      p.keys[at] = (int32_t)e.x;
+      p.perm[at] = (int32_t)e.y;
+    }
+  }
+}
+
+// ---- sums --------------------------------------------------------------------------------------------------------
+struct SumParams {
+  const void *g;
+  void *out;
+  int64_t V, D, g_stride, out_stride;
+  float scale;
+  int accumulate;
+  const int32_t *keys, *perm, *start;
+  float *part;     // [segments][2][D]: of the run that came from the segment before, of the one that goes on behind it
+  int64_t segs;
+  int seg;         // sorted positions of a segment
+  int64_t zero_ctas;
+  int zero_rows;   // rows of the table that a CTA looks at
+};
+
+constexpr int kSegMost = 128;
+constexpr int kRowsAhead = 8;  // rows of g under way per thread
+
+template <int DO, int N>
+__device__ __forceinline__ void finish(const SumParams &p, int64_t v, int64_t c, const float (&sum)[N]) {
+  typename Elem<DO>::T *dst = static_cast<typename Elem<DO>::T *>(p.out) + v * p.out_stride + c;
+  float r[N];
+  if (p.accumulate) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = fmaf(sum[i], p.scale, Elem<DO>::get(dst[i]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = sum[i] * p.scale;
+  }
+  store_n<DO, N>(dst, r);
+}
+
+// blockIdx.x: first the segments, then the CTAs that zero rows; blockIdx.y: columns.
+template <int DG, int DO, int N>
+__global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumParams p) {
+  __shared__ int32_t key[kSegMost + 2], row[kSegMost];
+  wait_for_stream_predecessor();
+  const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * N;
+  if ((int64_t)blockIdx.x >= p.segs) {
+    const int64_t v0 = ((int64_t)blockIdx.x - p.segs) * p.zero_rows, v1 = v0 + p.zero_rows < p.V ? v0 + p.zero_rows : p.V;
+    if (c >= p.D) return;
+    const float none[N] = {};
+    int32_t at = p.start[v0];
+    for (int64_t v = v0; v < v1; ++v) {
+      const int32_t next = p.start[v + 1];
+      if (next == at) store_n<DO, N>(static_cast<typename Elem<DO>::T *>(p.out) + v * p.out_stride + c, none);
+      at = next;
+    }
+    return;
+  }
+  const int64_t m = p.start[p.V];
+  const int64_t lo = (int64_t)blockIdx.x * p.seg;
+  if (lo >= m) return;
+  const int len = (int)(m - lo < p.seg ? m - lo : p.seg);
+  for (int i = threadIdx.x; i < len + 2; i += blockDim.x) {  // key[0]: before the segment, key[len + 1]: behind it
+    const int64_t at = lo - 1 + i;
+    key[i] = at >= 0 && at < m ? p.keys[at] : -1;
+    if (i >= 1 && i <= len) row[i - 1] = p.perm[at];
+  }
+  __syncthreads();
+  if (c >= p.D) return;
+  const typename Elem<DG>::T *const g = static_cast<const typename Elem<DG>::T *>(p.g) + c;
+  float sum[N] = {};
+  bool head = key[0] == key[1];  // the run in hand came from the segment before
+  for (int i0 = 0; i0 < len; i0 += kRowsAhead) {
+    float v[kRowsAhead][N];
+#pragma unroll
+    for (int k = 0; k < kRowsAhead; ++k)
+      if (i0 + k < len) load_n<DG, N>(g + (int64_t)(uint32_t)row[i0 + k] * p.g_stride, v[k]);
+#pragma unroll
+    for (int k = 0; k < kRowsAhead; ++k) {
+      const int i = i0 + k;
+      if (i >= len) break;
+#pragma unroll
+      for (int j = 0; j < N; ++j) sum[j] += v[k][j];
+      const int32_t own = key[i + 1];
+      if (own != key[i + 2] || i == len - 1) {
+        const bool on = own == key[i + 2];  // goes on behind the segment
+        if (head || on) {
+          store_n<0, N>(p.part + ((int64_t)blockIdx.x * 2 + (head ? 0 : 1)) * p.D + c, sum);
+        } else {
+          finish<DO, N>(p, own, c, sum);
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] = 0.f;
+        head = false;
+      }
+    }
+  }
+}
+
+// Runs of several segments: the CTA of the segment where one begins adds its parts in their order.
+template <int DO, int N>
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ SumParams p) {
+  wait_for_stream_predecessor();
+  const int64_t m = p.start[p.V];
+  const int64_t lo = (int64_t)blockIdx.x * p.seg, hi = lo + p.seg;
+  if (hi >= m) return;  // nothing behind this segment
+  const int32_t v = p.keys[hi - 1];
+  if (v != p.keys[hi] || p.start[v] < lo) return;
+  const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * N;
+  if (c >= p.D) return;
+  const int64_t last = (p.start[v + 1] - 1) / p.seg;  // segment of the run's end
+  const float *src = p.part + ((int64_t)blockIdx.x * 2 + 1) * p.D + c;
+  float sum[N];
+  load_n<0, N>(src, sum);
+  src = p.part + ((int64_t)blockIdx.x * 2 + 2) * p.D + c;
+#pragma unroll 8
+  for (int64_t s = blockIdx.x + 1; s <= last; ++s, src += 2 * p.D) {
+    float x[N];
+    load_n<0, N>(src, x);
+#pragma unroll
+    for (int j = 0; j < N; ++j) sum[j] += x[j];
+  }
+  finish<DO, N>(p, v, c, sum);
+}
+
+// ---- host side ---------------------------------------------------------------------------------------------------
+inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) != 0; }
+inline size_t esize_of(e3_dtype dt) { return dt == E3_F32 ? 4 : 2; }
+inline size_t up16(size_t b) { return (b + 15) / 16 * 16; }
+
+struct BackwardPlan {
+  int low, digits, tiles, seg;
+  int64_t tile, segs;
+  size_t counts, pairs, keys, perm, start, part, bytes;  // offsets into the workspace
+};
+BackwardPlan backward_plan(int64_t n, int64_t V, int64_t D) {
+  BackwardPlan b = {};
+  int bits = 1;
+  while ((int64_t(1) << bits) < V) ++bits;
+  b.low = (bits + 1) / 2 > bits - 10 ? (bits + 1) / 2 : bits - 10;
+  b.digits = (int)((V + (int64_t(1) << b.low) - 1) >> b.low);
+  // 2,048 tokens a tile, more where there would be over kTilesMost of them (every CTA of the second kernel reads all counts)
+  b.tile = (n + kTilesMost - 1) / kTilesMost;
+  b.tile = b.tile < 2048 ? 2048 : (b.tile + 255) / 256 * 256;
+  b.tiles = (int)((n + b.tile - 1) / b.tile);
+  b.seg = n < 32768 ? 32 : kSegMost;  // few tokens: more CTAs, many: fewer partial sums
+  b.segs = (n + b.seg - 1) / b.seg;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += up16(bytes);
+    return here;
+  };
+  b.counts = take((size_t)b.tiles * b.digits * 4);
+  b.pairs = take((size_t)n * 8);
+  b.keys = take((size_t)n * 4);
+  b.perm = take((size_t)n * 4);
+  b.start = take((size_t)(V + 1) * 4);
+  b.part = take((size_t)b.segs * 2 * D * 4);
+  b.bytes = at;
+  return b;
+}
+
+template <class... P, class... A>
+cudaError_t launch_behind(void (*kern)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, A &&...args) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
+template <int DG, int DO, int N>
+cudaError_t launch_sums(const SumParams &p, dim3 sums, dim3 joins, int threads, cudaStream_t stream) {
+  const cudaError_t e = launch_behind(sum_kernel<DG, DO, N>, sums, threads, 0, stream, p);
+  return e == cudaSuccess ? launch_behind(join_kernel<DO, N>, joins, threads, 0, stream, p) : e;
+}
+
+}  // namespace
+}  // namespace e3
+
+using namespace e3;
+
+extern "C" e3_status e3_embed_tokens(const int32_t *tok, int64_t n, const void *table, e3_dtype dt, int64_t V, int64_t D,
+                                     int64_t table_stride, float scale, void *out, int64_t out_stride, void *stream) {
+  if (dt != E3_F32 && dt != E3_BF16) return E3_ERR_DTYPE;
+  if (n < 0 || V < 1 || V >= (int64_t(1) << 31) || D < 1 || D >= (int64_t(1) << 31) || table_stride < D || out_stride < D)
+    return E3_ERR_INVALID_ARG;
+  if (n == 0) return E3_OK;
+  if (!tok || !table || !out) return E3_ERR_INVALID_ARG;
+  const size_t es = esize_of(dt);
+  if (misaligned(tok, 4) || misaligned(table, es) || misaligned(out, es)) return E3_ERR_ALIGNMENT;
+  EmbedParams p = {};
+  p.tok = tok; p.table = table; p.out = out; p.n = n; p.V = V; p.D = D; p.table_stride = table_stride; p.out_stride = out_stride;
+  p.scale = scale;
+  // rows that all begin on a 16-byte boundary move in vectors
+  const bool vec = !misaligned(table, 16) && !misaligned(out, 16) && table_stride * es % 16 == 0 && out_stride * es % 16 == 0 &&
+                   D * (int64_t)es >= 16;
+  const int64_t vecs = vec ? D / (int64_t)(16 / es) : D;
+  p.segs = (vecs + 32 * kEmbedVecs - 1) / (32 * kEmbedVecs);
+  p.len = (int)(((vecs + p.segs - 1) / p.segs + 31) / 32 * 32);
+  const int64_t ctas = (n * p.segs + kEmbedWarps - 1) / kEmbedWarps, most = 0x7fffffff;
+  const dim3 grid((unsigned)(ctas < most ? ctas : most));
+  const cudaError_t e = launch_behind(dt == E3_F32 ? (vec ? embed_kernel<0, 4> : embed_kernel<0, 1>) : (vec ? embed_kernel<1, 8> : embed_kernel<1, 1>),
+                                      grid, kEmbedWarps * 32, 0, static_cast<cudaStream_t>(stream), p);
+  return e == cudaSuccess ? E3_OK : E3_ERR_CUDA;
+}
+
+extern "C" size_t e3_embed_workspace_bytes(int64_t n, int64_t V, int64_t D) {
+  if (n <= 0 || n >= (int64_t(1) << 31) || V < 1 || V > kVMost || D < 1 || D >= kDMost) return 0;
+  return backward_plan(n, V, D).bytes;
+}
+
+extern "C" e3_status e3_embed_tokens_backward(const int32_t *tok, int64_t n, const void *g, e3_dtype dt, int64_t V, int64_t D,
+                                              int64_t g_stride, float scale, void *dtable, e3_dtype table_dt,
+                                              int64_t dtable_stride, int accumulate, void *workspace, size_t workspace_bytes,
+                                              void *stream) {
+  if ((dt != E3_F32 && dt != E3_BF16) || (table_dt != E3_F32 && table_dt != E3_BF16)) return E3_ERR_DTYPE;
+  if (n < 0 || n >= (int64_t(1) << 31) || V < 1 || V > kVMost || D < 1 || D >= kDMost || dtable_stride < D || (n > 0 && g_stride < D))
+    return E3_ERR_INVALID_ARG;
+  if (n == 0 && accumulate) return E3_OK;
+  if (!dtable || (n > 0 && (!tok || !g))) return E3_ERR_INVALID_ARG;
+  const size_t es = esize_of(dt), eo = esize_of(table_dt);
+  if (misaligned(tok, 4) || misaligned(g, es) || misaligned(dtable, eo) || misaligned(workspace, 16)) return E3_ERR_ALIGNMENT;
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  if (n == 0) {
+    const cudaError_t e = cudaMemset2DAsync(dtable, (size_t)dtable_stride * eo, 0, (size_t)D * eo, (size_t)V, cs);
+    return e == cudaSuccess ? E3_OK : E3_ERR_CUDA;
+  }
+  const BackwardPlan b = backward_plan(n, V, D);
+  if (!workspace || workspace_bytes < b.bytes) return E3_ERR_WORKSPACE;
+  char *const ws = static_cast<char *>(workspace);
+
+  SortParams s = {};
+  s.tok = tok; s.n = n; s.V = V; s.low = b.low; s.digits = b.digits; s.tiles = b.tiles; s.tile = b.tile;
+  s.counts = reinterpret_cast<int32_t *>(ws + b.counts);
+  s.pairs = reinterpret_cast<uint2 *>(ws + b.pairs);
+  s.keys = reinterpret_cast<int32_t *>(ws + b.keys);
+  s.perm = reinterpret_cast<int32_t *>(ws + b.perm);
+  s.start = reinterpret_cast<int32_t *>(ws + b.start);
+  cudaError_t e = launch_behind(count_kernel, dim3((unsigned)b.tiles), kCountThreads, 0, cs, s);
+  if (e == cudaSuccess)
+    e = launch_behind(scatter_kernel, dim3((unsigned)b.tiles), kScatterWarps * 32, (size_t)(kScatterWarps + 1) * b.digits * 4, cs, s);
+  if (e == cudaSuccess) {
+    // as many warps as have their own counters in 40 KB
+    int warps = (int)(40 * 1024 / 4 / (1 << b.low)) - 1;
+    warps = warps > 16 ? 16 : (warps < 1 ? 1 : warps);
+    e = launch_behind(bucket_kernel, dim3((unsigned)b.digits), warps * 32, (size_t)(warps + 1) * (1u << b.low) * 4, cs, s);
+  }
+  if (e != cudaSuccess) return E3_ERR_CUDA;
+
+  SumParams p = {};
+  p.g = g; p.out = dtable; p.V = V; p.D = D; p.g_stride = g_stride; p.out_stride = dtable_stride; p.scale = scale;
+  p.accumulate = accumulate != 0; p.keys = s.keys; p.perm = s.perm; p.start = s.start;
+  p.part = reinterpret_cast<float *>(ws + b.part); p.segs = b.segs; p.seg = b.seg;
+  // vectors of 16 bytes of the narrower type, if all rows begin on a 16-byte boundary and hold whole vectors
+  const int n_vec = dt == E3_BF16 || table_dt == E3_BF16 ? 8 : 4;
+  const bool vec = !misaligned(g, 16) && !misaligned(dtable, 16) && g_stride * es % 16 == 0 && dtable_stride * eo % 16 == 0 && D % n_vec == 0;
+  const int64_t vecs = vec ? D / n_vec : D;
+  const int64_t cols = (vecs + 255) / 256;
+  const int threads = (int)(((vecs + cols - 1) / cols + 31) / 32 * 32);
+  p.zero_rows = 32;
+  p.zero_ctas = accumulate ? 0 : (V + p.zero_rows - 1) / p.zero_rows;
+  const dim3 sums((unsigned)(b.segs + p.zero_ctas), (unsigned)cols), joins((unsigned)b.segs, (unsigned)cols);
+  if (dt == E3_F32 && table_dt == E3_F32)
+    e = vec ? launch_sums<0, 0, 4>(p, sums, joins, threads, cs) : launch_sums<0, 0, 1>(p, sums, joins, threads, cs);
+  else if (dt == E3_F32)
+    e = vec ? launch_sums<0, 1, 8>(p, sums, joins, threads, cs) : launch_sums<0, 1, 1>(p, sums, joins, threads, cs);
+  else if (table_dt == E3_F32)
+    e = vec ? launch_sums<1, 0, 8>(p, sums, joins, threads, cs) : launch_sums<1, 0, 1>(p, sums, joins, threads, cs);
+  else
+    e = vec ? launch_sums<1, 1, 8>(p, sums, joins, threads, cs) : launch_sums<1, 1, 1>(p, sums, joins, threads, cs);
+  return e == cudaSuccess ? E3_OK : E3_ERR_CUDA;
+}

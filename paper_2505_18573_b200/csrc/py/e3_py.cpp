@@ -482,6 +482,195 @@ PyObject *grpo_objective(PyObject *const *a) {
   return tuple_of({&out, &grad});
 }
 
+// ---- operators around the vocabulary: these run on the device of their first tensor, whichever is current ----------
+// The device of a call, current while it is made.
+struct OnDevice {
+  at::Device device;
+  c10::cuda::CUDAGuard guard;
+  explicit OnDevice(const at::Tensor &t) : device(t.device()), guard(t.device()) {}
+  void same(const at::Tensor *t, const char *name) const {
+    if (t && t->device() != device) {
+      PyErr_Format(PyExc_ValueError, "%s must be on the device of the other tensors", name);
+      throw PyFailed();
+    }
+  }
+};
+// A contiguous tensor of the type and number of entries that a call needs; nullptr stays nullptr.
+const at::Tensor *checked(const OnDevice &on, const at::Tensor *t, const char *name, at::ScalarType dtype, int64_t entries) {
+  if (!t) return t;
+  on.same(t, name);
+  if (!has_dtype(*t, dtype) || t->numel() != entries || !t->is_contiguous()) {
+    PyErr_Format(PyExc_ValueError, "%s must be a contiguous %s tensor with %lld entries", name, c10::toString(dtype), (long long)entries);
+    throw PyFailed();
+  }
+  return t;
+}
+Output checked_output(const OnDevice &on, PyObject *given, const char *name, bool make, at::IntArrayRef size, at::ScalarType dtype) {
+  int64_t n = 1;
+  for (int64_t s : size) n *= s;
+  checked(on, device_tensor(given, name), name, dtype, n);
+  return output(given, name, make, size, dtype, on.device);
+}
+// A matrix with a contiguous last dimension.
+struct Matrix {
+  void *data;
+  int64_t rows, cols, stride;
+};
+Matrix matrix_of(const OnDevice &on, const at::Tensor &t, const char *name) {
+  on.same(&t, name);
+  if (t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) {
+    PyErr_Format(PyExc_ValueError, "%s must be 2-D with a contiguous last dimension", name);
+    throw PyFailed();
+  }
+  Matrix m{t.data_ptr(), t.size(0), t.size(1), t.stride(0)};
+  if (m.rows <= 1 && m.stride < m.cols) m.stride = m.cols;
+  return m;
+}
+e3_dtype dtype_of(const at::Tensor &t, const char *name) {
+  if (has_dtype(t, at::kBFloat16)) return E3_BF16;
+  if (!has_dtype(t, at::kFloat)) {
+    PyErr_Format(PyExc_ValueError, "%s must be float32 or bfloat16", name);
+    throw PyFailed();
+  }
+  return E3_F32;
+}
+Scratch checked_scratch(const OnDevice &on, PyObject *given, size_t need, cudaStream_t stream) {
+  on.same(device_tensor(given, "workspace"), "workspace");
+  return scratch(given, need, on.device, stream);
+}
+
+PyObject *verify_drafts(PyObject *const *a) {
+  enum { kLogits, kTemps, kDraftTok, kUniforms, kDraftLen, kDraftLogits, kDraftTemps, kDraftLogp, kTok, kKept, kLogp, kEnt, kWantLogp, kWantEnt,
+         kWorkspace, kStream };
+  const at::Tensor &logits = required_tensor(a[kLogits], "logits");
+  const OnDevice on(logits);
+  const Logits l = logits_of(logits);
+  const at::Tensor &drafts = required_tensor(a[kDraftTok], "draft_tok");
+  if (drafts.dim() != 2) value_error("draft_tok must be 2-D, one row per sequence");
+  const int64_t n = drafts.size(0), k = drafts.size(1);
+  checked(on, &drafts, "draft_tok", at::kInt, n * k);
+  if (l.rows != n * (k + 1)) value_error("logits needs one row per draft and one more per sequence");
+  const at::Tensor &temps = *checked(on, &required_tensor(a[kTemps], "temps"), "temps", at::kFloat, n);
+  const at::Tensor *len = checked(on, device_tensor(a[kDraftLen], "draft_len"), "draft_len", at::kInt, n);
+  const at::Tensor &uniforms = required_tensor(a[kUniforms], "uniforms");
+  const Matrix u = matrix_of(on, uniforms, "uniforms");
+  if (!has_dtype(uniforms, at::kDouble) || u.rows != n || u.cols != k + (l.V + E3_SAMPLE_BLOCK - 1) / E3_SAMPLE_BLOCK + 1)
+    value_error("uniforms must be float64 [n_seq, drafts + ceil(V / 256) + 1]");
+  const at::Tensor *draft_logits = device_tensor(a[kDraftLogits], "draft_logits"), *draft_temps = nullptr, *draft_logp = nullptr;
+  Logits d{nullptr, l.dt, 0, 0, 0, on.device};
+  if (draft_logits) {
+    on.same(draft_logits, "draft_logits");
+    d = logits_of(*draft_logits);
+    if (d.dt != l.dt || d.V != l.V || d.rows != n * k) value_error("draft_logits needs one row per draft, of the width and dtype of logits");
+    draft_temps = checked(on, device_tensor(a[kDraftTemps], "draft_temps"), "draft_temps", at::kFloat, n);
+    draft_logp = checked(on, &required_tensor(a[kDraftLogp], "draft_logp"), "draft_logp", at::kFloat, n * k);
+  }
+  const Output tok = checked_output(on, a[kTok], "out_tok", true, {n, k + 1}, at::kInt);
+  const Output kept = checked_output(on, a[kKept], "out_kept", true, {n}, at::kInt);
+  const Output logp = checked_output(on, a[kLogp], "out_logp", truth(a[kWantLogp]), {n, k + 1}, at::kFloat);
+  const Output ent = checked_output(on, a[kEnt], "out_ent", truth(a[kWantEnt]), {n, k + 1}, at::kFloat);
+  const cudaStream_t stream = stream_of(a[kStream]);
+  const Scratch ws = checked_scratch(on, a[kWorkspace], e3_workspace_bytes(E3_CALL_VERIFY_DRAFTS, l.rows, 0, E3_F32), stream);
+  check("e3_verify_drafts", launch([&] {
+          return e3_verify_drafts(l.data, l.dt, n, k, l.V, l.stride, pointer<float>(temps), pointer<int32_t>(drafts), pointer<int32_t>(len),
+                                  draft_logits ? d.data : nullptr, d.stride, pointer<float>(draft_temps), pointer<float>(draft_logp),
+                                  static_cast<double *>(u.data), u.stride, tok.data<int32_t>(), kept.data<int32_t>(), logp.data<float>(),
+                                  ent.data<float>(), ws.data, ws.bytes, stream);
+        }));
+  return tuple_of({&tok, &kept, &logp, &ent});
+}
+
+PyObject *embed_tokens(PyObject *const *a) {
+  enum { kTable, kTok, kScale, kOut, kStream };
+  const at::Tensor &table = required_tensor(a[kTable], "table"), &tok = required_tensor(a[kTok], "tok");
+  const OnDevice on(table);
+  const Matrix t = matrix_of(on, table, "table");
+  const e3_dtype dt = dtype_of(table, "table");
+  checked(on, &tok, "tok", at::kInt, tok.numel());
+  const float scale = number(a[kScale]);
+  Output out;
+  Matrix o = {};
+  if (const at::Tensor *given = device_tensor(a[kOut], "out")) {
+    o = matrix_of(on, *given, "out");
+    if (!has_dtype(*given, table.scalar_type()) || o.rows != tok.numel() || o.cols != t.cols)
+      value_error("out needs one row per token, of the width and dtype of table");
+    out.object = a[kOut];
+    out.any = true;
+  } else {
+    c10::SmallVector<int64_t, 5> size(tok.sizes().begin(), tok.sizes().end());
+    size.push_back(t.cols);
+    out = output(a[kOut], "out", true, size, table.scalar_type(), on.device);
+    o.data = out.data<void>();
+    o.stride = t.cols;
+  }
+  const cudaStream_t stream = stream_of(a[kStream]);
+  check("e3_embed_tokens", launch([&] {
+          return e3_embed_tokens(pointer<int32_t>(tok), tok.numel(), t.data, dt, t.rows, t.cols, t.stride, scale, o.data, o.stride, stream);
+        }));
+  return out.release();
+}
+
+PyObject *embed_tokens_backward(PyObject *const *a) {
+  enum { kG, kTok, kV, kScale, kOut, kAccumulate, kDtype, kWorkspace, kStream };
+  const at::Tensor &grad = required_tensor(a[kG], "g"), &tok = required_tensor(a[kTok], "tok");
+  const OnDevice on(grad);
+  const Matrix g = matrix_of(on, grad, "g");
+  const e3_dtype dt = dtype_of(grad, "g");
+  checked(on, &tok, "tok", at::kInt, g.rows);
+  const int64_t V = static_cast<int64_t>(integer(a[kV]));
+  const float scale = number(a[kScale]);
+  const int accumulate = truth(a[kAccumulate]) ? 1 : 0, code = static_cast<int>(static_cast<int64_t>(integer(a[kDtype])));
+  const at::ScalarType type = code < 0 ? grad.scalar_type() : (code == E3_BF16 ? at::kBFloat16 : at::kFloat);
+  const at::Tensor *given = device_tensor(a[kOut], "out");
+  if (accumulate && !given) value_error("accumulate needs out");
+  if (given && code >= 0 && !has_dtype(*given, type)) value_error("out is not of that dtype");
+  if (!given && V < 1) check("e3_embed_tokens_backward", E3_ERR_INVALID_ARG);
+  const Output out = output(a[kOut], "out", true, {V, g.cols}, type, on.device);
+  const at::Tensor &table = given ? *given : out.made;
+  const Matrix o = matrix_of(on, table, "out");
+  const e3_dtype table_dt = dtype_of(table, "out");
+  if (o.rows != V || o.cols != g.cols) value_error("out must be [V, D]");
+  const cudaStream_t stream = stream_of(a[kStream]);
+  const Scratch ws = checked_scratch(on, a[kWorkspace], e3_embed_workspace_bytes(g.rows, V, g.cols), stream);
+  check("e3_embed_tokens_backward", launch([&] {
+          return e3_embed_tokens_backward(pointer<int32_t>(tok), g.rows, g.data, dt, V, g.cols, g.stride, scale, o.data, table_dt, o.stride,
+                                          accumulate, ws.data, ws.bytes, stream);
+        }));
+  return out.release();
+}
+
+PyObject *quantize(PyObject *const *a) {
+  enum { kX, kBlockRows, kQ, kScale, kStream };
+  const at::Tensor &x = required_tensor(a[kX], "x");
+  const OnDevice on(x);
+  const Matrix m = matrix_of(on, x, "x");
+  const e3_dtype dt = dtype_of(x, "x");
+  const int64_t block_rows = static_cast<int64_t>(integer(a[kBlockRows]));
+  if (block_rows != 1 && block_rows != E3_SCALE_BLOCK) value_error("block_rows must be 1 or 128");
+  const int64_t nr = (m.rows + block_rows - 1) / block_rows, nc = (m.cols + E3_SCALE_BLOCK - 1) / E3_SCALE_BLOCK;
+  Output q;
+  Matrix o = {};
+  if (const at::Tensor *given = device_tensor(a[kQ], "out_q")) {
+    o = matrix_of(on, *given, "out_q");
+    if (!has_dtype(*given, at::kFloat8_e4m3fn) || o.rows != m.rows || o.cols != m.cols) value_error("out_q must be float8_e4m3fn of the shape of x");
+    q.object = a[kQ];
+  } else {
+    const int64_t padded = (m.cols + 15) / 16 * 16;
+    q.made = empty({m.rows, padded}, at::kFloat8_e4m3fn, on.device);
+    if (padded != m.cols) q.made = q.made.narrow(1, 0, m.cols);
+    o.data = q.made.data_ptr();
+    o.stride = padded;
+  }
+  q.any = true;
+  const Output scale = checked_output(on, a[kScale], "out_scale", true, {nr, nc}, at::kFloat);
+  const cudaStream_t stream = stream_of(a[kStream]);
+  check("e3_quantize", launch([&] {
+          return e3_quantize(m.data, dt, m.rows, m.cols, m.stride, static_cast<int32_t>(block_rows), static_cast<uint8_t *>(o.data), o.stride,
+                             scale.data<float>(), nc, stream);
+        }));
+  return tuple_of({&q, &scale});
+}
+
 // ---- module ----------------------------------------------------------------------------------------------------
 template <PyObject *(*F)(PyObject *const *), int N>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -508,7 +697,8 @@ PyObject *set_error_class(PyObject *, PyObject *cls) {
 PyMethodDef g_methods[] = {
     E3_ENTRY(sample, 16), E3_ENTRY(token_logp_entropy, 13), E3_ENTRY(token_logp_entropy_backward, 11),
     E3_ENTRY(masked_mean_entropy, 5), E3_ENTRY(sequence_mean_entropy, 5), E3_ENTRY(masked_mean_entropy_static, 4),
-    E3_ENTRY(group_advantage, 8), E3_ENTRY(grpo_objective, 11), {"set_error_class", set_error_class, METH_O, nullptr},
+    E3_ENTRY(group_advantage, 8), E3_ENTRY(grpo_objective, 11), E3_ENTRY(verify_drafts, 16), E3_ENTRY(embed_tokens, 5),
+    E3_ENTRY(embed_tokens_backward, 9), E3_ENTRY(quantize, 5), {"set_error_class", set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
