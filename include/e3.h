@@ -283,6 +283,23 @@ E3_API e3_status e3_quantize(const void *x, e3_dtype dt, int64_t rows, int64_t c
                              uint8_t *q, int64_t q_stride, float *scale, int64_t scale_stride, void *stream);
 
 /*
+ * The vocabulary's projection in 8 bits, whose logits the row calls take: with the values and scales of e3_quantize (or any other fp32
+ * scales of the same layout)
+ *   logits[r, v] = sum_k x_scale[r, k] w_scale[v / E3_SCALE_BLOCK, k] sum_{i in block k of E3_SCALE_BLOCK columns} x[r, i] w[v, i].
+ * The products of a block are added in 32 bits, the blocks in fp32, and the logits rounded once.  For rollouts: there is no backward pass.
+ *
+ *   x, x_scale    device e4m3 bytes [rows, D], float [rows, ceil(D / E3_SCALE_BLOCK)]: the hidden states
+ *   w, w_scale    device e4m3 bytes [V, D], float [ceil(V / E3_SCALE_BLOCK), ceil(D / E3_SCALE_BLOCK)]: the table
+ *   logits        device, type dt, [rows, V] with row_stride elements from row to row; must not overlap the operands
+ *   out_status    device int32 or NULL: status word, see the conventions above (logits that a bounded wait left unfinished read NaN)
+ * x and w begin on a 16-byte boundary and their strides are multiples of 16 bytes (else E3_ERR_ALIGNMENT); what lies behind a row's D
+ * bytes is not looked at.  rows, V, D < 2^31 - 256.
+ */
+E3_API e3_status e3_project_vocab(const uint8_t *x, const float *x_scale, int64_t rows, int64_t x_stride, int64_t x_scale_stride,
+                                  const uint8_t *w, const float *w_scale, int64_t V, int64_t w_stride, int64_t w_scale_stride, int64_t D,
+                                  void *logits, e3_dtype dt, int64_t row_stride, int32_t *out_status, void *stream);
+
+/*
  * Batch entropy H_t of the scheduler (Sec. 4.2: "average entropy" of a batch), read as the mean
  * over all response tokens: out_mean = sum_j mask[j] ent[j] / sum_j mask[j], accumulated in
  * fp64 in a fixed order.  out_count = sum_j mask[j].  count == 0 gives mean NaN.

@@ -31,7 +31,8 @@ EXPORTS = ("e3_status_string", "e3_workspace_bytes", "e3_sample", "e3_token_logp
            "e3_masked_mean_entropy", "e3_masked_mean_entropy_static", "e3_group_advantage", "e3_allocate_budget", "e3_update_temperature",
            "e3_anneal_target", "e3_entropy_gap", "e3_update_temperature_gap", "e3_difficulty_accumulate", "e3_difficulty_rank", "e3_budget_curriculum",
            "e3_test_arm_stall", "e3_test_row_blocks", "e3_probe_read", "e3_sequence_mean_entropy",
-           "e3_verify_drafts", "e3_embed_tokens", "e3_embed_workspace_bytes", "e3_embed_tokens_backward", "e3_quantize")
+           "e3_verify_drafts", "e3_embed_tokens", "e3_embed_workspace_bytes", "e3_embed_tokens_backward", "e3_quantize",
+           "e3_project_vocab")
 
 
 class E3Error(RuntimeError):
@@ -135,6 +136,9 @@ def lib() -> C.CDLL:
         L.e3_quantize.restype = C.c_int
         L.e3_quantize.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int64,
                                   C.c_void_p, C.c_int64, C.c_void_p]
+        L.e3_project_vocab.restype = C.c_int
+        L.e3_project_vocab.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64,
+                                       C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_void_p]
         L.e3_test_row_blocks.restype = C.c_int32
         L.e3_test_row_blocks.argtypes = [C.c_int, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
         L.e3_test_arm_stall.restype = None
@@ -241,6 +245,13 @@ def e3_quantize(x, block_rows: int = 1, out_q=None, out_scale=None, stream=None)
     """``x`` [rows, cols] in 8 bits with a scale per ``block_rows`` x 128 entries (1 for hidden states, 128 for the vocabulary's table).
     Returns (q float8_e4m3fn [rows, cols], its rows 16-byte aligned, scale float32 [ceil(rows / block_rows), ceil(cols / 128)])."""
     return _nat.quantize(x, block_rows, out_q, out_scale, stream)
+
+
+def e3_project_vocab(x, x_scale, w, w_scale, dtype=None, out=None, status=None, stream=None):
+    """Logits [rows, V] of hidden states ``x`` [rows, D] and a table ``w`` [V, D] in float8_e4m3fn with the scales of :func:`e3_quantize`
+    (``block_rows`` 1 and 128).  ``dtype``: torch.bfloat16 (default) or torch.float32; ``status``: optional int32 CUDA tensor, the
+    device status word."""
+    return _nat.project_vocab(x, x_scale, w, w_scale, _dtype_code(dtype), out, status, stream)
 
 
 def e3_masked_mean_entropy(ent, mask=None, out=None, workspace=None, stream=None):

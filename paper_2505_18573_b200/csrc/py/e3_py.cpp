@@ -671,6 +671,39 @@ PyObject *quantize(PyObject *const *a) {
   return tuple_of({&q, &scale});
 }
 
+PyObject *project_vocab(PyObject *const *a) {
+  enum { kX, kXScale, kW, kWScale, kDtype, kOut, kStatus, kStream };
+  const at::Tensor &xt = required_tensor(a[kX], "x"), &wt = required_tensor(a[kW], "w");
+  const OnDevice on(xt);
+  if (!has_dtype(xt, at::kFloat8_e4m3fn) || !has_dtype(wt, at::kFloat8_e4m3fn)) value_error("x and w must be float8_e4m3fn");
+  Matrix x = matrix_of(on, xt, "x"), w = matrix_of(on, wt, "w");
+  if (x.cols != w.cols) value_error("x and w must have the same number of columns");
+  // (a single row has no stride of its own)
+  if (x.rows <= 1) x.stride = (x.cols + 15) / 16 * 16;
+  if (w.rows <= 1) w.stride = (w.cols + 15) / 16 * 16;
+  const at::Tensor &xs = required_tensor(a[kXScale], "x_scale"), &ws = required_tensor(a[kWScale], "w_scale");
+  const Matrix sx = matrix_of(on, xs, "x_scale"), sw = matrix_of(on, ws, "w_scale");
+  const int64_t nc = (x.cols + E3_SCALE_BLOCK - 1) / E3_SCALE_BLOCK;
+  if (!has_dtype(xs, at::kFloat) || !has_dtype(ws, at::kFloat) || sx.rows != x.rows || sx.cols != nc ||
+      sw.rows != (w.rows + E3_SCALE_BLOCK - 1) / E3_SCALE_BLOCK || sw.cols != nc)
+    value_error("x_scale must be float32 [rows, ceil(D / 128)], w_scale float32 [ceil(V / 128), ceil(D / 128)]");
+  const int code = static_cast<int>(static_cast<int64_t>(integer(a[kDtype])));
+  const at::Tensor *given = device_tensor(a[kOut], "out"), *status = device_tensor(a[kStatus], "status");
+  if (given && code >= 0 && !has_dtype(*given, code == E3_BF16 ? at::kBFloat16 : at::kFloat)) value_error("out is not of that dtype");
+  checked(on, status, "status", at::kInt, 1);
+  const Output out = output(a[kOut], "out", true, {x.rows, w.rows}, code == E3_F32 ? at::kFloat : at::kBFloat16, on.device);
+  const at::Tensor &logits = given ? *given : out.made;
+  const Matrix o = matrix_of(on, logits, "out");
+  const e3_dtype dt = dtype_of(logits, "out");
+  if (o.rows != x.rows || o.cols != w.rows) value_error("out must be [rows, V]");
+  const cudaStream_t stream = stream_of(a[kStream]);
+  check("e3_project_vocab", launch([&] {
+          return e3_project_vocab(static_cast<uint8_t *>(x.data), pointer<float>(xs), x.rows, x.stride, sx.stride, static_cast<uint8_t *>(w.data),
+                                  pointer<float>(ws), w.rows, w.stride, sw.stride, x.cols, o.data, dt, o.stride, pointer<int32_t>(status), stream);
+        }));
+  return out.release();
+}
+
 // ---- module ----------------------------------------------------------------------------------------------------
 template <PyObject *(*F)(PyObject *const *), int N>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -698,7 +731,8 @@ PyMethodDef g_methods[] = {
     E3_ENTRY(sample, 16), E3_ENTRY(token_logp_entropy, 13), E3_ENTRY(token_logp_entropy_backward, 11),
     E3_ENTRY(masked_mean_entropy, 5), E3_ENTRY(sequence_mean_entropy, 5), E3_ENTRY(masked_mean_entropy_static, 4),
     E3_ENTRY(group_advantage, 8), E3_ENTRY(grpo_objective, 11), E3_ENTRY(verify_drafts, 16), E3_ENTRY(embed_tokens, 5),
-    E3_ENTRY(embed_tokens_backward, 9), E3_ENTRY(quantize, 5), {"set_error_class", set_error_class, METH_O, nullptr},
+    E3_ENTRY(embed_tokens_backward, 9), E3_ENTRY(quantize, 5),
+    E3_ENTRY(project_vocab, 8), {"set_error_class", set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

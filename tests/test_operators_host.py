@@ -77,3 +77,16 @@ def test_embed_workspace(e3):
 def test_quantize_refuses(e3, change, status):
     a = dict(x=P, dt=e3.E3_F32, rows=4, cols=300, row_stride=300, block_rows=1, q=P, q_stride=304, scale=P, scale_stride=3, stream=None)
     assert e3.lib().e3_quantize(*{**a, **change}.values()) == (0 if status is None else getattr(e3, "E3_ERR_" + status))
+
+
+@pytest.mark.parametrize("change, status", [
+    (dict(dt=7), "DTYPE"), (dict(rows=-1), "INVALID_ARG"), (dict(V=0), "INVALID_ARG"), (dict(D=0), "INVALID_ARG"), (dict(x_stride=192), "INVALID_ARG"),
+    (dict(w_stride=192), "INVALID_ARG"), (dict(x_scale_stride=1), "INVALID_ARG"), (dict(w_scale_stride=1), "INVALID_ARG"),
+    (dict(row_stride=499), "INVALID_ARG"), (dict(V=1 << 31, row_stride=1 << 31), "INVALID_ARG"), (dict(x=None), "INVALID_ARG"),
+    (dict(x_scale=None), "INVALID_ARG"), (dict(w=None), "INVALID_ARG"), (dict(w_scale=None), "INVALID_ARG"), (dict(logits=None), "INVALID_ARG"),
+    (dict(x=P + 8), "ALIGNMENT"), (dict(w=P + 8), "ALIGNMENT"), (dict(x_stride=216), "ALIGNMENT"), (dict(w_stride=216), "ALIGNMENT"),
+    (dict(x_scale=P + 2), "ALIGNMENT"), (dict(logits=P + 1), "ALIGNMENT"), (dict(out_status=P + 2), "ALIGNMENT"), (dict(rows=0, x=None), None)])
+def test_project_refuses(e3, change, status):
+    a = dict(x=P, x_scale=P, rows=3, x_stride=208, x_scale_stride=2, w=P, w_scale=P, V=500, w_stride=208, w_scale_stride=2, D=200, logits=P,
+             dt=e3.E3_BF16, row_stride=500, out_status=None, stream=None)
+    assert e3.lib().e3_project_vocab(*{**a, **change}.values()) == (0 if status is None else getattr(e3, "E3_ERR_" + status))
