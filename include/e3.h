@@ -98,8 +98,8 @@ E3_API const char *e3_status_string(e3_status s);
 
 /* Bytes of device scratch a call uses for the given problem size.  For
  * E3_CALL_MASKED_MEAN_ENTROPY `rows` is the number of tokens n, for E3_CALL_GRPO_OBJECTIVE the number of
- * responses n_seq, for E3_CALL_SEQUENCE_MEAN_ENTROPY the number of sequences n_seq, for E3_CALL_VERIFY_DRAFTS the number of
- * logits rows n_seq * (max_draft + 1); V, dt are ignored for these.  E3_CALL_SAMPLE: 256 KiB for the partial states of cut rows plus
+ * responses n_seq, for E3_CALL_SEQUENCE_MEAN_ENTROPY the number of sequences n_seq; V, dt are ignored for these.
+ * For E3_CALL_VERIFY_DRAFTS `rows` is the number of logits rows n_seq * (max_draft + 1).  E3_CALL_SAMPLE: 256 KiB for the partial states of cut rows plus
  * room for the sums of blocks (about 1/32 of the bytes of the logits), which the present kernels leave untouched;
  * E3_CALL_TOKEN_LOGP_ENTROPY: 256 KiB plus the partial sums of the fused mean entropy.
  * Scratch contents on entry never matter.  A workspace must not be shared by calls that can run
@@ -228,9 +228,10 @@ E3_API e3_status e3_token_logp_entropy_backward(const void *logits, e3_dtype dt,
  *   out_kept      device int32 [n_seq]: a
  *   out_logp, out_ent   device float [n_seq, max_draft + 1], each may be NULL: log-probability of the emitted token under p_j, entropy
  *                 of p_j; 0 behind the drawn token
- *   workspace     e3_workspace_bytes(E3_CALL_VERIFY_DRAFTS, n_seq * (max_draft + 1), 0, 0) bytes of device scratch
+ *   workspace     e3_workspace_bytes(E3_CALL_VERIFY_DRAFTS, n_seq * (max_draft + 1), V, dt) bytes of device scratch
  * A position that is reached and whose row holds NaN or +inf or nothing but -inf, whose temperature is negative or not finite, or whose
- * uniform lies outside [0, 1) ends the sequence: token -1, log-probability and entropy NaN.  n_seq * (max_draft + 1) < 2^26.
+ * uniform lies outside [0, 1) (of the block uniforms: any) ends the sequence: token -1, log-probability and entropy NaN.  n_seq * (max_draft + 1) < 2^26,
+ * V < 2^31 - 2^16.
  */
 E3_API e3_status e3_verify_drafts(const void *logits, e3_dtype dt, int64_t n_seq, int64_t max_draft, int64_t V, int64_t row_stride,
                                   const float *temps, const int32_t *draft_tok, const int32_t *draft_len,

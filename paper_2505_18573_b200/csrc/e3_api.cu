@@ -9,7 +9,7 @@
 
 namespace e3 {
 size_t grpo_workspace_bytes(int64_t n_seq);
-size_t verify_workspace_bytes(int64_t rows);
+size_t verify_workspace_bytes(int64_t rows, int64_t V);
 }
 
 namespace {
@@ -46,7 +46,7 @@ extern "C" size_t e3_workspace_bytes(e3_call which, int64_t rows, int64_t V, e3_
     case E3_CALL_MASKED_MEAN_ENTROPY: return e3::mean_workspace_bytes(rows < 0 ? 0 : rows);
     case E3_CALL_GRPO_OBJECTIVE: return e3::grpo_workspace_bytes(rows);
     case E3_CALL_SEQUENCE_MEAN_ENTROPY: return e3::seq_mean_workspace_bytes(rows);
-    case E3_CALL_VERIFY_DRAFTS: return e3::verify_workspace_bytes(rows);
+    case E3_CALL_VERIFY_DRAFTS: return e3::verify_workspace_bytes(rows, V);
   }
   return 0;
 }

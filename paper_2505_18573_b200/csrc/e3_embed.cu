@@ -39,27 +39,49 @@ struct Elem<1> {
   static __device__ __forceinline__ T put(float v) { return __float2bfloat16_rn(v); }  // one rounding, to nearest even
 };
 
-// N consecutive elements (N = a 16-byte vector of them, or 1).
+// N consecutive elements as they lie in memory (N = one or two 16-byte vectors of them, or 1).
 template <int DT, int N>
-__device__ __forceinline__ void load_n(const typename Elem<DT>::T *p, float (&v)[N]) {
+struct Raw {
+  uint4 v[N / Elem<DT>::kVec];
+};
+template <int DT>
+struct Raw<DT, 1> {
+  typename Elem<DT>::T v;
+};
+template <int DT, int N>
+__device__ __forceinline__ Raw<DT, N> load_raw(const typename Elem<DT>::T *p) {
+  Raw<DT, N> r;
   if constexpr (N == 1) {
-    v[0] = Elem<DT>::get(*p);
+    r.v = *p;
   } else {
 #pragma unroll
-    for (int k = 0; k < N; k += Elem<DT>::kVec) {
-      const uint4 w = *reinterpret_cast<const uint4 *>(p + k);
-      const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+    for (int k = 0; k < N / Elem<DT>::kVec; ++k) r.v[k] = reinterpret_cast<const uint4 *>(p)[k];
+  }
+  return r;
+}
+template <int DT, int N>
+__device__ __forceinline__ void values(const Raw<DT, N> &r, float (&x)[N]) {
+  if constexpr (N == 1) {
+    x[0] = Elem<DT>::get(r.v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < N / Elem<DT>::kVec; ++k) {
+      const uint32_t w[4] = {r.v[k].x, r.v[k].y, r.v[k].z, r.v[k].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (DT == 0) {
-          v[k + i] = __uint_as_float(x[i]);
+          x[k * 4 + i] = __uint_as_float(w[i]);
         } else {
-          v[k + 2 * i] = __uint_as_float(x[i] << 16);
-          v[k + 2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
+          x[k * 8 + 2 * i] = __uint_as_float(w[i] << 16);
+          x[k * 8 + 2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
         }
       }
     }
   }
+}
+template <int DT, int N>
+__device__ __forceinline__ void load_n(const typename Elem<DT>::T *p, float (&v)[N]) {
+  values<DT, N>(load_raw<DT, N>(p), v);
 }
 template <int DT, int N>
 __device__ __forceinline__ void store_n(typename Elem<DT>::T *p, const float (&v)[N]) {
@@ -104,7 +126,7 @@ constexpr int kEmbedVecs = 4;  // vectors under way per lane
 
 // A warp takes a piece of a row: bound by the two moves of the row through memory; the token's number has to come first.
 template <int DT, int N>
-__global__ void __launch_bounds__(kEmbedWarps * 32) embed_kernel(const __grid_constant__ EmbedParams p) {
+__global__ void __launch_bounds__(kEmbedWarps * 32, N == 1 ? 4 : 8) embed_kernel(const __grid_constant__ EmbedParams p) {
   using E = Elem<DT>;
   wait_for_stream_predecessor();
   const int lane = threadIdx.x & 31;
@@ -119,16 +141,18 @@ __global__ void __launch_bounds__(kEmbedWarps * 32) embed_kernel(const __grid_co
     const typename E::T *src = static_cast<const typename E::T *>(p.table) + (live ? tok : 0) * p.table_stride;
     typename E::T *dst = static_cast<typename E::T *>(p.out) + t * p.out_stride;
     for (int64_t c = c0 + lane * N; c < c1; c += 32 * N * kEmbedVecs) {
-      float v[kEmbedVecs][N];
+      Raw<DT, N> v[kEmbedVecs];
 #pragma unroll
       for (int k = 0; k < kEmbedVecs; ++k)
-        if (live && c + k * 32 * N < c1) load_n<DT, N>(src + c + k * 32 * N, v[k]);
+        if (live && c + k * 32 * N < c1) v[k] = load_raw<DT, N>(src + c + k * 32 * N);
 #pragma unroll
       for (int k = 0; k < kEmbedVecs; ++k) {
         if (c + k * 32 * N >= c1) break;
+        float x[N];
+        values<DT, N>(v[k], x);
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[k][i] = live ? v[k][i] * p.scale : fill;
-        store_n<DT, N>(dst + c + k * 32 * N, v[k]);
+        for (int i = 0; i < N; ++i) x[i] = live ? x[i] * p.scale : fill;
+        store_n<DT, N>(dst + c + k * 32 * N, x);
       }
     }
     // entries behind the last whole vector
@@ -400,16 +424,18 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumPar
   float sum[N] = {};
   bool head = key[0] == key[1];  // the run in hand came from the segment before
   for (int i0 = 0; i0 < len; i0 += kRowsAhead) {
-    float v[kRowsAhead][N];
+    Raw<DG, N> v[kRowsAhead];
 #pragma unroll
     for (int k = 0; k < kRowsAhead; ++k)
-      if (i0 + k < len) load_n<DG, N>(g + (int64_t)(uint32_t)row[i0 + k] * p.g_stride, v[k]);
+      if (i0 + k < len) v[k] = load_raw<DG, N>(g + (int64_t)(uint32_t)row[i0 + k] * p.g_stride);
 #pragma unroll
     for (int k = 0; k < kRowsAhead; ++k) {
       const int i = i0 + k;
       if (i >= len) break;
+      float x[N];
+      values<DG, N>(v[k], x);
 #pragma unroll
-      for (int j = 0; j < N; ++j) sum[j] += v[k][j];
+      for (int j = 0; j < N; ++j) sum[j] += x[j];
       const int32_t own = key[i + 1];
       if (own != key[i + 2] || i == len - 1) {
         const bool on = own == key[i + 2];  // goes on behind the segment

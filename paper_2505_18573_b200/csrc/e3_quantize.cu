@@ -23,37 +23,51 @@ struct QuantParams {
   int64_t row_blocks, col_blocks;
 };
 
-// Eight entries of a row from column c on, as 32-bit patterns of their values in fp32; 0 from `left` on.
+// Eight entries of a row from column c on, as they lie in memory; 0 from `left` on.
+template <int DT>
+struct Raw {
+  uint4 v[DT == 0 ? 2 : 1];
+};
 template <int DT, bool VEC>
-__device__ __forceinline__ void load8(const char *row, int64_t c, int64_t left, uint32_t (&v)[8]) {
-  if (DT == 1) {
-    if (VEC && left >= 8) {
-      const uint4 w = *reinterpret_cast<const uint4 *>(row + c * 2);
-      const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+__device__ __forceinline__ Raw<DT> load8(const char *row, int64_t c, int64_t left) {
+  Raw<DT> r;
+  if (VEC && left >= 8) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = x[i] << 16;
-        v[2 * i + 1] = x[i] & 0xFFFF0000u;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i < left ? (uint32_t)reinterpret_cast<const uint16_t *>(row)[c + i] << 16 : 0u;
-    }
-  } else if (VEC && left >= 8) {
-    const uint4 a = *reinterpret_cast<const uint4 *>(row + c * 4), b = *reinterpret_cast<const uint4 *>(row + c * 4 + 16);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? reinterpret_cast<const uint32_t *>(row)[c + i] : 0u;
+    for (int k = 0; k < (DT == 0 ? 2 : 1); ++k) r.v[k] = __ldcs(reinterpret_cast<const uint4 *>(row + c * (DT == 0 ? 4 : 2)) + k);
+    return r;
   }
-}
-// |x| as patterns: they order like the values, NaN above infinity.
-__device__ __forceinline__ uint32_t most8(const uint32_t (&v)[8]) {
-  uint32_t m = 0u;
+  uint32_t w[8];
+  if (DT == 1) {
+    const uint16_t *const p = reinterpret_cast<const uint16_t *>(row) + c;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, v[i] & 0x7FFFFFFFu);
-  return m;
+    for (int i = 0; i < 4; ++i) w[i] = (2 * i < left ? p[2 * i] : 0u) | (2 * i + 1 < left ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+  } else {
+    const uint32_t *const p = reinterpret_cast<const uint32_t *>(row) + c;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = i < left ? p[i] : 0u;
+  }
+#pragma unroll
+  for (int k = 0; k < (DT == 0 ? 2 : 1); ++k) r.v[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+  return r;
+}
+template <int DT>
+__device__ __forceinline__ float entry(const Raw<DT> &r, int i) {
+  const uint4 &v = r.v[DT == 0 ? i >> 2 : 0];
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  if (DT == 0) return __uint_as_float(w[i & 3]);
+  return __uint_as_float((i & 1) != 0 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+}
+// Largest |x|, as a pattern of fp32: they order like the values, NaN above infinity.
+template <int DT>
+__device__ __forceinline__ uint32_t most8(const Raw<DT> &r) {
+  if (DT == 0) {
+    uint32_t m = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(entry(r, i)) & 0x7FFFFFFFu);
+    return m;
+  }
+  const uint32_t m = __vmaxu2(__vmaxu2(r.v[0].x & 0x7FFF7FFFu, r.v[0].y & 0x7FFF7FFFu), __vmaxu2(r.v[0].z & 0x7FFF7FFFu, r.v[0].w & 0x7FFF7FFFu));
+  return max(m & 0xFFFF0000u, m << 16);
 }
 // Scale of a block, and its inverse, from the pattern of its largest |x|.
 __device__ __forceinline__ float scale_of(uint32_t most, float &inverse) {
@@ -71,15 +85,15 @@ __device__ __forceinline__ float scale_of(uint32_t most, float &inverse) {
   inverse = __uint_as_float((uint32_t)(254 - e) << 23);
   return __uint_as_float((uint32_t)e << 23);
 }
-__device__ __forceinline__ uint32_t four(const uint32_t *v, float inverse) {
-  const float2 lo = make_float2(__uint_as_float(v[0]) * inverse, __uint_as_float(v[1]) * inverse);
-  const float2 hi = make_float2(__uint_as_float(v[2]) * inverse, __uint_as_float(v[3]) * inverse);
+template <int DT>
+__device__ __forceinline__ uint32_t four(const Raw<DT> &r, int i, float inverse) {
+  const float2 lo = make_float2(entry(r, i) * inverse, entry(r, i + 1) * inverse), hi = make_float2(entry(r, i + 2) * inverse, entry(r, i + 3) * inverse);
   const uint32_t a = __nv_cvt_float2_to_fp8x2(lo, __NV_SATFINITE, __NV_E4M3), b = __nv_cvt_float2_to_fp8x2(hi, __NV_SATFINITE, __NV_E4M3);
   return a | b << 16;
 }
-template <bool VEC>
-__device__ __forceinline__ void store8(uint8_t *q, int64_t left, const uint32_t (&v)[8], float inverse) {
-  const uint2 w = make_uint2(four(v, inverse), four(v + 4, inverse));
+template <int DT, bool VEC>
+__device__ __forceinline__ void store8(uint8_t *q, int64_t left, const Raw<DT> &r, float inverse) {
+  const uint2 w = make_uint2(four(r, 0, inverse), four(r, 4, inverse));
   if (VEC && left >= 8) {
     *reinterpret_cast<uint2 *>(q) = w;
   } else {
@@ -104,8 +118,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) quantize_rows_kernel(const __g
   const int64_t row = item / p.col_blocks, cb = item - row * p.col_blocks;
   const bool live = row < p.rows;
   const int64_t c = cb * kBlock + lane * 8, left = live ? p.cols - c : 0;
-  uint32_t v[8];
-  load8<DT, VEC>(static_cast<const char *>(p.x) + (live ? row : 0) * p.x_stride * (DT == 0 ? 4 : 2), c, left, v);
+  const Raw<DT> v = load8<DT, VEC>(static_cast<const char *>(p.x) + (live ? row : 0) * p.x_stride * (DT == 0 ? 4 : 2), c, left);
   uint32_t most = most8(v);
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
@@ -113,26 +126,26 @@ __global__ void __launch_bounds__(kRowWarps * 32) quantize_rows_kernel(const __g
   float inverse;
   const float scale = scale_of(most, inverse);
   if (lane == 0) p.scale[row * p.scale_stride + cb] = scale;
-  store8<VEC>(p.q + row * p.q_stride + c, left, v, inverse);
+  store8<DT, VEC>(p.q + row * p.q_stride + c, left, v, inverse);
 }
 
 // Tables: a CTA takes a block of 128 x 128, 16 lanes a row of it, eight rows each.
 constexpr int kTableThreads = 256;
 constexpr int kEach = kBlock * 16 / kTableThreads;
 template <int DT, bool VEC>
-__global__ void __launch_bounds__(kTableThreads) quantize_table_kernel(const __grid_constant__ QuantParams p) {
+__global__ void __launch_bounds__(kTableThreads, DT == 0 ? 2 : 4) quantize_table_kernel(const __grid_constant__ QuantParams p) {
   __shared__ uint32_t sh[kTableThreads / 32];
   wait_for_stream_predecessor();
   const int sub = threadIdx.x >> 4, lane = threadIdx.x & 15;
   const int64_t item = blockIdx.x, rb = item / p.col_blocks, cb = item - rb * p.col_blocks;
   const int64_t c = cb * kBlock + lane * 8;
-  uint32_t v[kEach][8];
+  Raw<DT> v[kEach];
   uint32_t most = 0u;
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
     const int64_t row = rb * kBlock + k * (kTableThreads / 16) + sub;
     const bool live = row < p.rows;
-    load8<DT, VEC>(static_cast<const char *>(p.x) + (live ? row : 0) * p.x_stride * (DT == 0 ? 4 : 2), c, live ? p.cols - c : 0, v[k]);
+    v[k] = load8<DT, VEC>(static_cast<const char *>(p.x) + (live ? row : 0) * p.x_stride * (DT == 0 ? 4 : 2), c, live ? p.cols - c : 0);
   }
 #pragma unroll
   for (int k = 0; k < kEach; ++k) most = max(most, most8(v[k]));
@@ -147,7 +160,7 @@ __global__ void __launch_bounds__(kTableThreads) quantize_table_kernel(const __g
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
     const int64_t row = rb * kBlock + k * (kTableThreads / 16) + sub;
-    if (row < p.rows) store8<VEC>(p.q + row * p.q_stride + c, p.cols - c, v[k], inverse);
+    if (row < p.rows) store8<DT, VEC>(p.q + row * p.q_stride + c, p.cols - c, v[k], inverse);
   }
 }
 

@@ -3,39 +3,41 @@
 // p_j = softmax(z_j / tau) of the target at position j, q_j the draft's distribution there.  Draft d_j is kept iff u_j q_j(d_j) < p_j(d_j);
 // at the first position a that is refused the token comes from max(p_a - q_a, 0), behind a sequence whose drafts were all kept from p_a.
 //
-// Two passes.  verify_rows_kernel takes the rows position by position (every sequence's first row, then every second, ...), a row in parts
-// of equal length, one CTA each: the part's largest logit R, Z = sum 2^t and W = sum 2^t (z - R) with t = (z - R) log2(e) / tau.  The CTA that
-// comes last to a row joins the parts in their order and decides; rows behind a refused position are not read any more once that is known
-// (which changes no result).  draw_kernel gives every sequence a cluster of CTAs that reads the one row (and the draft's) the token comes from.
+// One pass over the logits and a draw that looks at a few blocks.  verify_rows_kernel takes the rows position by position (every sequence's
+// first row, then every second, ...), a row in parts of equal length, one CTA each: the sum of 2^t of every block of 256 entries, t = (z - R) log2(e) /
+// tau with a logit R that the warp has met and nothing lies far above, and over the part Z = sum 2^t and W = sum 2^t t.  The CTA that comes last to a row joins the parts
+// in their order and decides; rows behind a refused position are not read any more once that is known (which changes no result).
 //
-// The token comes from the construction of the blocked sampler with given uniforms, one per block of 256 entries: the block with the largest
-// ln(sum r_i) - ln(-ln u_b), then the first entry in it whose prefix sum exceeds v times its sum.  Two tokens are the same only if every
-// comparison falls the same way, so each is made with a bound on the error of fp32 sums; what the bound does not settle (a few in
-// 10,000) is taken again in fp64, over the whole row.
+// The token comes from the construction of the blocked sampler with given uniforms, one per block: the block with the largest
+// ln(sum r_i) - ln(-ln u_b), then the first entry in it whose prefix sum exceeds v times its sum.  r = p needs nothing but the blocks' sums;
+// r = p - q is at most p, so draw_kernel takes the block with the largest score of p, and looks at the others whose score of p reaches that
+// block's own score: three or four of them as a rule.  (Reading the row and the draft's row again, 512 x 151,936, took 164 us.)
+//
+// Two tokens are the same only if every comparison falls the same way, so each is made with a bound on the error of fp32 sums; what the
+// bound does not settle (a few in 10,000) is taken again in fp64.
 #include "e3_rows_device.cuh"
 
-#include <cooperative_groups.h>
-
-#include <atomic>
+#include <mutex>
+#include <type_traits>
 
 #include "e3.h"
-
-namespace cg = cooperative_groups;
 
 namespace e3 {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kPartsMost = 32;
-constexpr int kClusterMost = 8;
 constexpr unsigned kAll = 0xffffffffu;
-// Relative error of p and q, as sums over a block in fp32 (2^t: 2^-22 and the rounding of t) and through Z.
+constexpr float kFarBelow = 3e38f;    // distances below the largest logit are no larger (-inf: weight 0, and 0 times its distance is 0)
+constexpr float kFarFrom = 0x1p20f;    // |R log2(e) / tau| from which t is taken from z - R
+constexpr float kSoundSum = 0x1p20f;   // a lane's sum from which a higher reference is taken
+constexpr int kScoresKept = 2048;  // blocks whose scores of p stay in shared memory
+// Relative error of sums of p and q over a block in fp32 (2^t: 2^-22 and the rounding of t) and through Z, and of Z.
 constexpr float kSumError = 5e-6f;
 constexpr float kSumErrorPerBit = 1.5e-7f;  // per factor of two by which the sum, or the draft's own q, lies below 1 (rounding of t)
-constexpr double kZError = 1e-5;
+constexpr double kZError = 3e-6;  // (sums of at most forty roundings one after the other, 2^-24 each, 2^t: 2^-22)
 
-enum : int { kKept = 0, kRefused = 1, kInvalid = 2 };
+enum : int { kKept = 0, kRefused = 1, kInvalid = 2, kNear = 3 };  // kNear: u q is closer to p than Z is known; kept for the time being
 
 struct VerifyPart {
   float R, Z, W;
@@ -64,7 +66,8 @@ struct VerifyParams {
   int32_t *first, *arrived;  // workspace: first position not kept, parts of a row that have come
   VerifyRow *rows;
   VerifyPart *parts;
-  int n_parts, part;  // parts of a row, entries of one
+  float2 *sums;       // of every row's blocks: sum of 2^t, the logit R it refers to
+  int n_parts, part;  // parts of a row, blocks of one
 };
 
 __device__ __forceinline__ void wait_for_stream_predecessor() {
@@ -122,19 +125,20 @@ __global__ void __launch_bounds__(256) begin_kernel(const __grid_constant__ Veri
   }
 }
 
-// Entries of a vector outside [0, n) become -inf; the vector's first entry has number e.
-template <int DT>
-__device__ __forceinline__ uint4 keep_entries(const uint4 &v, int e, int n) {
+// Entries of a vector outside [lo, hi) become -inf, or (FINITE) -1e30, whose product with its weight 0 is 0; the vector's first entry has number e.
+template <int DT, bool FINITE>
+__device__ __forceinline__ uint4 keep_entries(const uint4 &v, int e, int lo, int hi) {
+  constexpr uint32_t kFill = FINITE ? (DT == 0 ? 0xF149F2CAu : 0xF14AF14Au) : (DT == 0 ? 0xFF800000u : 0xFF80FF80u);
   constexpr int kE = DT == 0 ? 4 : 8;
-  if (e >= 0 && e + kE <= n) return v;
+  if (e >= lo && e + kE <= hi) return v;
   uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (DT == 0) {
-      if (e + i < 0 || e + i >= n) w[i] = 0xFF800000u;
+      if (e + i < lo || e + i >= hi) w[i] = kFill;
     } else {
-      if (e + 2 * i < 0 || e + 2 * i >= n) w[i] = (w[i] & 0xFFFF0000u) | 0xFF80u;
-      if (e + 2 * i + 1 < 0 || e + 2 * i + 1 >= n) w[i] = (w[i] & 0xFFFFu) | 0xFF800000u;
+      if (e + 2 * i < lo || e + 2 * i >= hi) w[i] = (w[i] & 0xFFFF0000u) | (kFill & 0xFFFFu);
+      if (e + 2 * i + 1 < lo || e + 2 * i + 1 >= hi) w[i] = (w[i] & 0xFFFFu) | (kFill & 0xFFFF0000u);
     }
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
@@ -161,22 +165,51 @@ __device__ __forceinline__ float most_of(const uint4 &v) {
 struct Sums {
   float R, Z, W;
 };
-// Joins two sums; either may be empty (R = -inf).
+// Joins two sums; either may be empty (R = -inf, Z = 0).
 __device__ __forceinline__ void join(Sums &a, float R, float Z, float W, float c) {
   const float m = fmaxf(a.R, R);
   if (m == -CUDART_INF_F) return;
-  const float da = a.R > -CUDART_INF_F ? fmaxf(a.R - m, -1e30f) : -1e30f, db = R > -CUDART_INF_F ? fmaxf(R - m, -1e30f) : -1e30f;
-  const float fa = a.Z > 0.f ? ex2f(da * c) : 0.f, fb = Z > 0.f ? ex2f(db * c) : 0.f;
+  const float da = fmaxf((a.R - m) * c, -kFarBelow), db = fmaxf((R - m) * c, -kFarBelow);
+  const float fa = a.Z > 0.f ? ex2f(da) : 0.f, fb = Z > 0.f ? ex2f(db) : 0.f;
   a.W = (fa > 0.f ? fa * fmaf(da, a.Z, a.W) : 0.f) + (fb > 0.f ? fb * fmaf(db, Z, W) : 0.f);
   a.Z = fa * a.Z + fb * Z;
   a.R = m;
+}
+// Joins the sums of the first N lanes (empty ones: R = -inf, Z = 0) in a fixed order, for all of these lanes.
+template <int N>
+__device__ __forceinline__ void join_lanes(Sums &s, float c) {
+  const float m = dec_float(__reduce_max_sync(kAll, enc_float(s.R)));
+  if (m == -CUDART_INF_F) return;
+  const float d = fmaxf((s.R - m) * c, -kFarBelow), f = s.Z > 0.f ? ex2f(d) : 0.f;
+  s.W = f > 0.f ? f * fmaf(d, s.Z, s.W) : 0.f;
+  s.Z *= f;
+  s.R = m;
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1) {
+    s.Z += __shfl_xor_sync(kAll, s.Z, o);
+    s.W += __shfl_xor_sync(kAll, s.W, o);
+  }
+}
+// Largest logit of the warp and its lowest index.
+__device__ __forceinline__ void best_of_warp(float &R, int &best) {
+  const float m = dec_float(__reduce_max_sync(kAll, enc_float(R)));
+  best = __reduce_min_sync(kAll, R == m ? best : INT_MAX);
+  R = m;
 }
 
 // sum over the row of exp((z - R) / tau) in fp64, of the entries from `from` on in steps of `step`, by one thread.
 template <int DT>
 __device__ __noinline__ double exact_terms(const char *row, int V, float R, float tau, int from, int step) {
+  constexpr int kAhead = 8;
+  const double beta = 1.0 / (double)tau;
   double s = 0.0;
-  for (int i = from; i < V; i += step) s += exp(((double)load_elem<DT>(row, i) - (double)R) / (double)tau);
+  for (int64_t i0 = from; i0 < V; i0 += (int64_t)step * kAhead) {
+    float z[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) z[k] = i0 + (int64_t)k * step < V ? load_elem<DT>(row, i0 + (int64_t)k * step) : -CUDART_INF_F;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) s += exp(((double)z[k] - (double)R) * beta);
+  }
   return s;
 }
 __device__ __forceinline__ double block_sum(double v, double *sh /* [warps] */) {
@@ -191,123 +224,351 @@ __device__ __forceinline__ double block_sum(double v, double *sh /* [warps] */) 
   return v;
 }
 
-template <int DT>
-__global__ void __launch_bounds__(kThreads, 4) verify_rows_kernel(const __grid_constant__ VerifyParams p) {
-  constexpr int kE = DT == 0 ? 4 : 8;  // entries of a vector
-  constexpr int kEsize = DT == 0 ? 4 : 2;
-  constexpr int kAhead = 8;            // vectors under way per thread
-  __shared__ Sums sh[kWarps];
-  __shared__ int sh_best[kWarps], sh_bad[kWarps];
-  __shared__ double sh_sum[kWarps];
-  __shared__ int sh_flag;
-  __shared__ VerifyRow sh_row;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int64_t item = blockIdx.x;
-  const int64_t at = item / p.n_parts;
-  const int part = (int)(item - at * p.n_parts);
-  const int64_t j = at / p.n_seq, b = at - j * p.n_seq, r = b * (p.drafts + 1) + j;
-  wait_for_stream_predecessor();
-  const int len = length_of(p, b);
-  if (j > len) return;
-  if (j > 0 && __syncthreads_or(tid == 0 && *(volatile const int32_t *)(p.first + b) < j)) return;
+// Sums over the warp of kB values at once: lane l gets that of value l / (32 / kB).
+template <int kB>
+__device__ __forceinline__ float warp_sums(float (&v)[kB]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int n = kB, o = 16; o > 0; o >>= 1) {
+    if (n > 1) {
+      n >>= 1;
+      const bool upper = (lane & o) != 0;
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        const float keep = upper ? v[i + n] : v[i], give = upper ? v[i] : v[i + n];
+        v[i] = keep + __shfl_xor_sync(kAll, give, o);
+      }
+    } else {
+      v[0] += __shfl_xor_sync(kAll, v[0], o);
+    }
+  }
+  return v[0];
+}
 
-  const char *const row = p.logits + r * p.row_bytes;
-  const float tau = p.temps[b];
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+template <int DT>
+struct Form {
+  static constexpr int kEsize = DT == 0 ? 4 : 2;
+  static constexpr int kE = 16 / kEsize;              // entries of a vector
+  static constexpr int kN = 8 / kE;                   // vectors of a lane in a block
+  static constexpr int kStep = DT == 0 ? 2 : 4;       // blocks that a warp takes at a time: 2 KB
+  static constexpr int kPartMost = DT == 0 ? 24 : 48;  // blocks that a CTA holds: 24 KB
+};
+constexpr int kRowWarps = 4, kRowThreads = kRowWarps * 32;
+constexpr int kHeld = 8;  // CTAs that an SM holds
+// Shared memory of a warp with `blocks` blocks: whole steps (the last one is read as a whole), and a vector behind them for rows that begin anywhere.
+template <int DT>
+__host__ __device__ constexpr int warp_bytes(int blocks) {
+  return (blocks + Form<DT>::kStep - 1) / Form<DT>::kStep * Form<DT>::kStep * E3_SAMPLE_BLOCK * Form<DT>::kEsize + 16;
+}
+// Waits until at most `later` of the thread's groups of copies are under way.
+__device__ __forceinline__ void copies_wait(int later) {
+  switch (later) {
+    case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+    case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+    case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+    default: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+  }
+}
+
+// Sums of a lane's entries of kStep blocks: z of each, and W over all, t = z c - M.  CAREFUL: t = (z - R) c, and entries far below R (-inf) have
+// weight 0 and count as finite.  lone: entries of rows that begin off a vector.
+template <int DT, bool CAREFUL>
+__device__ __forceinline__ float step_sums(const uint4 (&v)[Form<DT>::kStep][Form<DT>::kN], const float (&lone)[Form<DT>::kStep], bool lones,
+                                           float c, float R, float M, float (&z)[Form<DT>::kStep]) {
+  constexpr int kE = Form<DT>::kE, kN = Form<DT>::kN, kStep = Form<DT>::kStep;
+  const f2 c2 = pack2f(c, c), nR2 = pack2f(-R, -R), nM2 = pack2f(-M, -M);
+  f2 W2 = pack2f(0.f, 0.f);
+#pragma unroll
+  for (int k = 0; k < kStep; ++k) {
+    f2 Z2 = pack2f(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+#pragma unroll
+      for (int h = 0; h < kE / 2; ++h) {
+        f2 t = pair_of<DT>(v[k][i], h);
+        if (CAREFUL) {
+          t = mul2(add2(t, nR2), c2);
+          t = pack2f(fmaxf(t.x, -kFarBelow), fmaxf(t.y, -kFarBelow));
+        } else {
+          t = fma2(t, c2, nM2);
+        }
+        const f2 e = pack2f(ex2f(t.x), ex2f(t.y));
+        Z2 = add2(Z2, e);
+        W2 = fma2(e, t, W2);
+      }
+    }
+    z[k] = sum2(Z2);
+  }
+  float W = sum2(W2);
+  if (lones) {
+#pragma unroll
+    for (int k = 0; k < kStep; ++k) {
+      const float t = fmaxf(CAREFUL ? (lone[k] - R) * c : fmaf(lone[k], c, -M), -kFarBelow), e = ex2f(t);
+      z[k] += e;
+      W = fmaf(e, t, W);
+    }
+  }
+  return W;
+}
+
+// Largest entry of a step; NaN if one is.
+template <int DT>
+__device__ __forceinline__ float most_of_step(const uint4 (&v)[Form<DT>::kStep][Form<DT>::kN], const float (&lone)[Form<DT>::kStep]) {
+  float m = -CUDART_INF_F;
+#pragma unroll
+  for (int k = 0; k < Form<DT>::kStep; ++k) {
+#pragma unroll
+    for (int i = 0; i < Form<DT>::kN; ++i) m = max_nan(m, most_of<DT>(v[k][i]));
+    m = max_nan(m, lone[k]);
+  }
+  return m;
+}
+
+// A part of a row, by its number: parts of a row run fastest, then sequences, then positions.
+struct Place {
+  int64_t r, b;
+  int j, part;
+};
+__device__ __forceinline__ Place place_of(const VerifyParams &p, uint32_t item) {
+  const uint32_t at = item / (uint32_t)p.n_parts, j = at / (uint32_t)p.n_seq, b = at - j * (uint32_t)p.n_seq;
+  return Place{(int64_t)b * (p.drafts + 1) + j, (int64_t)b, (int)j, (int)(item - at * (uint32_t)p.n_parts)};
+}
+
+// Joins the parts of row r and decides its position, by a warp.
+template <int DT>
+__device__ __noinline__ void decide(const VerifyParams &p, int64_t r, int64_t b, int j, float tau, float c) {
+  const int lane = threadIdx.x & 31;
+  const bool greedy = tau == 0.f;
+  Draft d = {kNoDraft, -1, 0.f, 0.f, 0.0};
+  float zd = 0.f;
+  double u = 0.0;
+  if (lane == 0 && j < length_of(p, b)) {
+    d = draft_of<DT>(p, b, j);
+    u = p.uniforms[b * p.u_stride + j];
+    if (d.kind != kNoDraft) zd = load_elem<DT>(p.logits + r * p.row_bytes, d.tok);
+  }
+  Sums s = {-CUDART_INF_F, 0.f, 0.f};
+  int best = INT_MAX;
+  bool bad = false;
+  for (int i = lane; i < p.n_parts; i += 32) {  // (written by other SMs: from L2)
+    const int4 *const src = reinterpret_cast<const int4 *>(p.parts + r * p.n_parts + i);
+    const int4 x = __ldcg(src), y = __ldcg(src + 1);
+    const float R = __int_as_float(x.x);
+    bad |= x.w != 0;
+    if (greedy) {
+      if (R > s.R || (R == s.R && y.x < best)) {
+        s.R = R;
+        best = y.x;
+      }
+    } else {
+      join(s, R, __int_as_float(x.y), __int_as_float(x.z), c);
+    }
+  }
+  bad = __any_sync(kAll, bad);
+  if (greedy) best_of_warp(s.R, best);
+  else join_lanes<32>(s, c);
+  if (lane != 0) return;
+  VerifyRow w = {0.0, s.R, 0.f, 0.f, kRefused, best, 0};
+  if (bad || !(s.R > -CUDART_INF_F) || (!greedy && !(s.Z > 0.f)) || !usable_uniform(u)) {
+    w.state = kInvalid;
+  } else if (greedy) {
+    if (d.kind != kNoDraft && d.tok == best && u * exp(d.lnq) < 1.0) w.state = kKept;
+  } else {
+    // c is log2(e) / tau rounded to fp32: that turns t by as much, and ln Z by the mean of t
+    const double beta = 1.0 / (double)tau, mean = (double)__fdiv_rn(s.W, s.Z) * kLn2, lnZ = log((double)s.Z);
+    w.lnZ = lnZ + (beta / (kLn2 * (double)c) - 1.0) * mean;
+    w.ent = (float)fmax(lnZ - mean, 0.0);
+    if (d.kind != kNoDraft) {
+      const double lp = ((double)zd - (double)s.R) * beta - w.lnZ;
+      const double ratio = u * exp(d.lnq - lp);  // (a token of probability 0: infinity or, from u = 0, NaN)
+      w.logp = (float)lp;
+      w.state = fabs(ratio - 1.0) < 2.0 * kZError ? kNear : (ratio < 1.0 ? kKept : kRefused);
+    }
+  }
+  p.rows[r] = w;
+  if (w.state == kRefused || w.state == kInvalid) {
+    __threadfence();
+    atomicMin(p.first + b, (int32_t)j);
+  }
+}
+
+// Bound by the exponentials' and the other instructions' issue (70 for a lane's eight logits) and by latency: a CTA of four warps takes a part of up to
+// 24 KB, all of it under way at once, eight of them an SM.  Larger CTAs wait longer for their last warp and for the decision; warps that run on from part
+// to part without a barrier (three steps of 2 KB under way each) were slower for their fences and read a third more rows that were not wanted.
+template <int DT>
+__global__ void __launch_bounds__(kRowThreads, kHeld) verify_rows_kernel(const __grid_constant__ VerifyParams p) {
+  using F = Form<DT>;
+  constexpr int kE = F::kE, kN = F::kN, kEsize = F::kEsize, kStep = F::kStep;
+  extern __shared__ __align__(16) unsigned char dyn[];
+  __shared__ Sums sh[kRowWarps];
+  __shared__ int sh_best[kRowWarps], sh_bad[kRowWarps];
+  const int lane = threadIdx.x & 31, warp = __shfl_sync(kAll, threadIdx.x >> 5, 0);
+  const Place at = place_of(p, blockIdx.x);
+  wait_for_stream_predecessor();
+  const int len = length_of(p, at.b);
+  const float tau = p.temps[at.b];
+  // (no position before it is refused; all warps see the same)
+  if (at.j > len || (at.j > 0 && __syncthreads_or(threadIdx.x == 0 && *(volatile const int32_t *)(p.first + at.b) < at.j))) return;
+  const char *const row = p.logits + at.r * p.row_bytes;
+  const int skip = (int)(reinterpret_cast<uintptr_t>(row) & 15u) / kEsize;
   const bool greedy = tau == 0.f, usable = greedy || (tau > 0.f && tau < CUDART_INF_F);
   const float c = greedy || !usable ? 0.f : __fdiv_rn(kLog2e, tau);
-  const int e0 = part * p.part, n = p.V - e0 < p.part ? p.V - e0 : p.part;
+  // the warp's blocks: `each` of every round of the CTA
+  const int round = p.part < F::kPartMost ? p.part : F::kPartMost, each = (round + kRowWarps - 1) / kRowWarps;
+  const int begin = at.part * p.part, end = begin + p.part < p.blocks ? begin + p.part : p.blocks;
+  const uint32_t mem = smem_addr(dyn) + (uint32_t)(warp * warp_bytes<DT>(each));
   Sums s = {-CUDART_INF_F, 0.f, 0.f};
+  float M = CUDART_INF_F, f = 1.f, g = 0.f;  // R c rounded, what that does to t (g = M - R c) and to 2^t
+  auto refer_to = [&](float m) {  // refers the sums to the largest m of the warp, if that lies above R
+    m = dec_float(__reduce_max_sync(kAll, enc_float(m)));
+    if (m > s.R) {
+      if (s.R > -CUDART_INF_F) {
+        const float d = fmaxf((s.R - m) * c, -kFarBelow), t = ex2f(d);
+        s.W = t * fmaf(d, s.Z, s.W);
+        s.Z *= t;
+      }
+      s.R = m;
+      M = m * c;
+      g = fabsf(M) < kFarFrom ? fmaf(-m, c, M) : 0.f;
+      f = ex2f(g);
+    }
+  };
   bool bad = !usable || !(c < CUDART_INF_F);
   int best = INT_MAX;
-  if (usable) {
-    const char *const begin = row + (int64_t)e0 * kEsize;
-    const int a = (int)(reinterpret_cast<uintptr_t>(begin) & 15u), skip = a / kEsize;
-    const uint4 *const src = reinterpret_cast<const uint4 *>(begin - a);
-    const int vecs = (skip + n + kE - 1) / kE;
-    f2 Z2 = pack2f(0.f, 0.f), W2 = Z2;
-    for (int i0 = tid; i0 < vecs; i0 += kThreads * kAhead) {
-      uint4 v[kAhead];
+  // A lane's entries of a block are 8 consecutive ones of the vectors that begin at the row's last 16-byte boundary: `skip` entries early, so that
+  // the first lane leaves out as many and the block's last ones are taken by the first lanes, one each.
+#pragma unroll 1
+  for (int first = begin + warp * each; first < end; first += kRowWarps * each) {
+    const int count = first + each < end ? each : end - first, steps = (count + kStep - 1) / kStep;
+    __syncwarp();  // (what lay there has been read)
+    {
+      const char *src = row - skip * kEsize + (int64_t)first * (E3_SAMPLE_BLOCK * kEsize) + lane * 16;
+      const int64_t whole = (int64_t)(p.V - first * E3_SAMPLE_BLOCK + skip) * kEsize;  // bytes up to the row's end
+      const int blocks = count * E3_SAMPLE_BLOCK * kEsize + (skip != 0 ? 16 : 0);       // (and the vector behind them)
+      int left = (int)(whole < blocks ? whole : blocks) - lane * 16;                    // from this lane's next vector on
+      uint32_t dst = mem + (uint32_t)lane * 16u;
+      constexpr int kVecs = kStep * kN;
+#pragma unroll 1
+      for (int k = 0; k < steps; ++k) {
+        if (left > 512 * (kVecs - 1)) {
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const int i = i0 + k * kThreads;
-        if (i < vecs) v[k] = __ldcs(src + i);
-      }
-      float m = -CUDART_INF_F;
+          for (int i = 0; i < kVecs; ++i) copy16(dst + (uint32_t)(i * 512), src + i * 512);
+        } else {
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const int i = i0 + k * kThreads;
-        if (i < vecs) {
-          v[k] = keep_entries<DT>(v[k], i * kE - skip, n);
-          m = max_nan(m, most_of<DT>(v[k]));
+          for (int i = 0; i < kVecs; ++i)
+            if (left > i * 512) copy16(dst + (uint32_t)(i * 512), src + i * 512);
         }
+        src += kVecs * 512;
+        dst += kVecs * 512;
+        left -= kVecs * 512;
+        if (k == steps - 1 && left > 0 && lane == 0) copy16(dst, src);
+        asm volatile("cp.async.commit_group;" ::: "memory");
       }
-      bad |= !(m < CUDART_INF_F);
+    }
+    float2 *const sums = p.sums + at.r * p.blocks + first;
+#pragma unroll 1
+    for (int k0 = 0; k0 < count; k0 += kStep) {
+      // (rows that begin off a vector: a block's last entries lie in the next block's first vector)
+      copies_wait(skip != 0 ? 0 : steps - 1 - k0 / kStep);
+      __syncwarp();
+      const uint32_t slot = mem + (uint32_t)(k0 * E3_SAMPLE_BLOCK * kEsize);
+      uint4 v[kStep][kN];
+      float lone[kStep];
+      const bool whole = skip == 0 && k0 + kStep <= count && (first + k0 + kStep) * E3_SAMPLE_BLOCK <= p.V;
+#pragma unroll
+      for (int k = 0; k < kStep; ++k) {
+        lone[k] = -1e30f;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) v[k][i] = lds128(slot + (uint32_t)(((k * 32 + lane) * kN + i) * 16));
+      }
+      auto cut = [&](auto finite) {  // what is not the blocks' or not the row's
+#pragma unroll
+        for (int k = 0; k < kStep; ++k) {
+          const int lo = (first + k0 + k) * E3_SAMPLE_BLOCK, hi = k0 + k < count ? p.V : 0;
+#pragma unroll
+          for (int i = 0; i < kN; ++i) v[k][i] = keep_entries<DT, decltype(finite)::value>(v[k][i], lo + lane * 8 + i * kE - skip, lo, hi);
+          if (!(lane < skip && lo + E3_SAMPLE_BLOCK - skip + lane < hi)) lone[k] = decltype(finite)::value ? -1e30f : -CUDART_INF_F;
+        }
+      };
+      if (skip != 0) {
+#pragma unroll
+        for (int k = 0; k < kStep; ++k)
+          if (lane < skip) lone[k] = lds_elem<DT>(slot + (uint32_t)(((k + 1) * E3_SAMPLE_BLOCK + lane) * kEsize));
+      }
+      if (!whole) cut(std::true_type());
       if (greedy) {
+        cut(std::false_type());
+        const float m = most_of_step<DT>(v, lone);
+        bad |= !(m < CUDART_INF_F);
         if (m > s.R) {
           s.R = m;
-          best = -1;
-        }
-        if (best < 0) {  // lowest entry of this round with that logit
+          best = INT_MAX;
 #pragma unroll
-          for (int k = kAhead - 1; k >= 0; --k) {
-            const int i = i0 + k * kThreads;
-            if (i < vecs) {
+          for (int k = 0; k < kStep; ++k) {  // lowest of the lane's entries with that logit (those of later steps have higher numbers)
+            const int lo = (first + k0 + k) * E3_SAMPLE_BLOCK;
 #pragma unroll
-              for (int h = kE / 2 - 1; h >= 0; --h) {
-                const f2 z = pair_of<DT>(v[k], h);
-                if (z.y == m) best = e0 + i * kE - skip + 2 * h + 1;
-                if (z.x == m) best = e0 + i * kE - skip + 2 * h;
+            for (int i = 0; i < kN; ++i) {
+#pragma unroll
+              for (int h = 0; h < kE / 2; ++h) {
+                const f2 z = pair_of<DT>(v[k][i], h);
+                const int e = lo + lane * 8 + i * kE - skip + 2 * h;
+                if (z.x == m && e < best) best = e;
+                if (z.y == m && e + 1 < best) best = e + 1;
               }
             }
+            if (lone[k] == m && lo + E3_SAMPLE_BLOCK - skip + lane < best) best = lo + E3_SAMPLE_BLOCK - skip + lane;
           }
-          if (best < 0) best = INT_MAX;  // (NaN: the row is invalid)
         }
         continue;
       }
-      if (!(m > -CUDART_INF_F)) continue;
-      if (m > s.R) {
-        if (s.R > -CUDART_INF_F) {
-          const float d = fmaxf(s.R - m, -1e30f), f = ex2f(d * c);
-          const f2 d2 = pack2f(d, d), f2f = pack2f(f, f);
-          W2 = mul2(f2f, fma2(d2, Z2, W2));
-          Z2 = mul2(f2f, Z2);
-        }
-        s.R = m;
+      float z[kStep], W = 0.f, all = 0.f;
+      bool sound = false;
+      if (s.R == -CUDART_INF_F) {  // a first reference: the largest logit of one block
+        const float m = most_of<DT>(v[0][0]);
+        refer_to(m > -1e29f && m < CUDART_INF_F ? m : -CUDART_INF_F);
       }
-      const f2 nR = pack2f(-s.R, -s.R), c2 = pack2f(c, c);
+      if (fabsf(M) < kFarFrom && c > 1e-20f) {  // (there is a reference, and -1e30 lies far below it)
+        W = step_sums<DT, false>(v, lone, skip != 0, c, s.R, M, z);
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        if (i0 + k * kThreads < vecs) {
-#pragma unroll
-          for (int h = 0; h < kE / 2; ++h) {
-            f2 d = add2(pair_of<DT>(v[k], h), nR);
-            d = pack2f(fmaxf(d.x, -1e30f), fmaxf(d.y, -1e30f));  // (-inf: weight 0, and 0 times its distance is 0)
-            const f2 t = mul2(d, c2), e = pack2f(ex2f(t.x), ex2f(t.y));
-            Z2 = add2(Z2, e);
-            W2 = fma2(e, d, W2);
-          }
-        }
+        for (int k = 0; k < kStep; ++k) all += z[k];
+        sound = !__any_sync(kAll, !(all < kSoundSum) || !(fabsf(W) < kFarBelow));
       }
+      if (!sound) {
+        // no reference yet, or a logit far above it, NaN or an infinity
+        cut(std::false_type());
+        float m = most_of_step<DT>(v, lone);
+        if (!(m < CUDART_INF_F)) {
+          bad = true;
+          m = -CUDART_INF_F;
+        }
+        refer_to(m);
+        W = step_sums<DT, true>(v, lone, skip != 0, c, s.R > -CUDART_INF_F ? s.R : 0.f, 0.f, z);
+        all = 0.f;
+#pragma unroll
+        for (int k = 0; k < kStep; ++k) all += z[k];
+        s.Z += all;
+        s.W += W;
+      } else {  // from M, which is rounded, to R c
+        s.Z = fmaf(f, all, s.Z);
+        s.W = fmaf(f, fmaf(g, all, W), s.W);
+      }
+      const float sum = warp_sums(z);
+      const int k = k0 + lane / (32 / kStep);
+      if (lane % (32 / kStep) == 0 && k < count) sums[k] = make_float2(sound ? sum * f : sum, s.R > -CUDART_INF_F ? s.R : 0.f);
     }
-    s.Z = sum2(Z2);
-    s.W = sum2(W2);
   }
   // ---- the part's result, joined in a fixed order
   if (greedy) {
+    best_of_warp(s.R, best);
+  } else {  // (R is that of the warp)
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-      const float R = __shfl_xor_sync(kAll, s.R, o);
-      const int i = __shfl_xor_sync(kAll, best, o);
-      if (R > s.R || (R == s.R && i < best)) {
-        s.R = R;
-        best = i;
-      }
-    }
-  } else {
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const float R = __shfl_xor_sync(kAll, s.R, o), Z = __shfl_xor_sync(kAll, s.Z, o), W = __shfl_xor_sync(kAll, s.W, o);
-      join(s, R, Z, W, c);
+      s.Z += __shfl_xor_sync(kAll, s.Z, o);
+      s.W += __shfl_xor_sync(kAll, s.W, o);
     }
   }
   bad = __any_sync(kAll, bad);
@@ -317,94 +578,21 @@ __global__ void __launch_bounds__(kThreads, 4) verify_rows_kernel(const __grid_c
     sh_bad[warp] = bad;
   }
   __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < kWarps; ++w) {
-      if (greedy) {
-        if (sh[w].R > s.R || (sh[w].R == s.R && sh_best[w] < best)) {
-          s.R = sh[w].R;
-          best = sh_best[w];
-        }
-      } else {
-        join(s, sh[w].R, sh[w].Z, sh[w].W, c);
-      }
-      bad |= sh_bad[w] != 0;
-    }
+  if (warp != 0) return;
+  s = lane < kRowWarps ? sh[lane] : Sums{-CUDART_INF_F, 0.f, 0.f};
+  best = lane < kRowWarps ? sh_best[lane] : INT_MAX;
+  bad = __any_sync(kAll, lane < kRowWarps && sh_bad[lane] != 0);
+  if (greedy) best_of_warp(s.R, best);
+  else join_lanes<kRowWarps>(s, c);
+  int last = 0;
+  if (lane == 0) {
     VerifyPart out = {s.R, s.Z, s.W, bad ? 1 : 0, best, {0, 0, 0}};
-    p.parts[r * p.n_parts + part] = out;
-    __threadfence();
-    sh_flag = atomicAdd(p.arrived + r, 1) == p.n_parts - 1;
-    __threadfence();
+    p.parts[at.r * p.n_parts + at.part] = out;
+    int before;
+    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(p.arrived + at.r) : "memory");
+    last = before == p.n_parts - 1;
   }
-  __syncthreads();
-  if (!sh_flag) return;
-
-  // ---- the last CTA of the row: all parts are there
-  Draft d = {kNoDraft, -1, 0.f, 0.f, 0.0};
-  if (j < len) d = draft_of<DT>(p, b, j);
-  if (warp == 0) {
-    VerifyPart q = {-CUDART_INF_F, 0.f, 0.f, 0, INT_MAX, {0, 0, 0}};
-    if (lane < p.n_parts) {  // (written by other SMs: from L2)
-      const int4 *const src = reinterpret_cast<const int4 *>(p.parts + r * p.n_parts + lane);
-      const int4 x = __ldcg(src), y = __ldcg(src + 1);
-      q.R = __int_as_float(x.x); q.Z = __int_as_float(x.y); q.W = __int_as_float(x.z); q.err = x.w;
-      q.best = y.x;
-    }
-    s = {q.R, q.Z, q.W};
-    best = q.best;
-    bad = __any_sync(kAll, q.err != 0);
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const float R = __shfl_xor_sync(kAll, s.R, o), Z = __shfl_xor_sync(kAll, s.Z, o), W = __shfl_xor_sync(kAll, s.W, o);
-      const int i = __shfl_xor_sync(kAll, best, o);
-      if (greedy) {
-        if (R > s.R || (R == s.R && i < best)) {
-          s.R = R;
-          best = i;
-        }
-      } else {
-        join(s, R, Z, W, c);
-      }
-    }
-    if (lane == 0) {
-      VerifyRow w = {0.0, s.R, 0.f, 0.f, kRefused, best, 0};
-      const double u = j < len ? p.uniforms[b * p.u_stride + j] : 0.0;
-      bool near = false;
-      if (bad || !(s.R > -CUDART_INF_F) || (!greedy && !(s.Z > 0.f)) || !usable_uniform(u)) {
-        w.state = kInvalid;
-      } else if (greedy) {
-        if (d.kind != kNoDraft && d.tok == best && u * exp(d.lnq) < 1.0) w.state = kKept;
-      } else {
-        w.lnZ = log((double)s.Z);
-        w.ent = (float)fmax(w.lnZ - (double)s.W / ((double)s.Z * (double)tau), 0.0);
-        if (d.kind != kNoDraft) {
-          const double x = ((double)load_elem<DT>(row, d.tok) - (double)s.R) / (double)tau, lp = x - w.lnZ;
-          const double ratio = u * exp(d.lnq - lp);  // (a token of probability 0: infinity or, from u = 0, NaN)
-          w.logp = (float)lp;
-          w.state = ratio < 1.0 ? kKept : kRefused;
-          near = fabs(ratio - 1.0) < kZError;
-        }
-      }
-      sh_row = w;
-      sh_flag = near;
-    }
-  }
-  __syncthreads();
-  if (sh_flag) {  // u q and p are closer than Z is known
-    const double total = block_sum(exact_terms<DT>(row, p.V, sh_row.R, tau, tid, kThreads), sh_sum);
-    if (tid == 0) {
-      sh_row.lnZ = log(total);
-      const double lp = ((double)load_elem<DT>(row, d.tok) - (double)sh_row.R) / (double)tau - sh_row.lnZ;
-      sh_row.logp = (float)lp;
-      sh_row.state = p.uniforms[b * p.u_stride + j] * exp(d.lnq) < exp(lp) ? kKept : kRefused;
-    }
-  }
-  if (tid == 0) {
-    p.rows[r] = sh_row;
-    if (sh_row.state != kKept) {
-      __threadfence();
-      atomicMin(p.first + b, (int32_t)j);
-    }
-  }
+  if (__shfl_sync(kAll, last, 0) != 0) decide<DT>(p, at.r, at.b, at.j, tau, c);
 }
 
 // ---- second pass ---------------------------------------------------------------------------------------------------
@@ -450,10 +638,11 @@ __device__ __forceinline__ float gumbel_of(double u) {
 
 // The row a token is drawn from.
 struct DrawRow {
-  const char *z, *y;   // target, draft (kDistribution)
+  const char *z, *y;      // target, draft (kDistribution)
   int V, kind, d;
-  float tau, R, y_d, tau_d;
-  double lnZ, lnq;
+  float tau, R, y_d;
+  double lnZ, lnq, beta, beta_d;  // (betas: 1 / temperature)
+  float c, nz, cd, nq;    // the same for sums in fp32, log2 units
 };
 // The eight entries from i on (i a multiple of 8; a block's entries of a lane) as vectors, whatever the row's alignment.
 template <int DT>
@@ -491,331 +680,413 @@ __device__ __forceinline__ float entry(const Eight<DT> &e, int k) {
 
 // Weight max(p - q, 0) of an entry in fp64 (q of a logit that is NaN: the entry is not drawn); mass: p.
 __device__ __forceinline__ double exact_weight(const DrawRow &w, int kind, int i, float z, float y, double &mass) {
-  mass = exp(((double)z - (double)w.R) / (double)w.tau - w.lnZ);
+  mass = exp(((double)z - (double)w.R) * w.beta - w.lnZ);
   if (kind == kNoDraft) return mass;
   if (kind == kOneHot) return i == w.d ? 0.0 : mass;
-  return fmax(mass - exp(((double)y - (double)w.y_d) / (double)w.tau_d + w.lnq), 0.0);
+  return fmax(mass - exp(((double)y - (double)w.y_d) * w.beta_d + w.lnq), 0.0);
 }
 
-// Draw inside block b by a warp.  False: the fp32 normaliser leaves open which entry it is.
+// Draw inside block b by the CTA, an entry a thread (a warp with eight entries a lane took 8 us: the exponentials are in fp64).  False: the fp32
+// normaliser leaves open which entry it is.
 template <int DT>
-__device__ __noinline__ bool draw_in(const DrawRow &w, int kind, int b, double u, bool exact, int &tok) {
+__device__ __noinline__ bool draw_in(const DrawRow &w, int kind, int b, double u, bool exact, double *sh /* [2 * warps] */, int &tok) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, i = b * E3_SAMPLE_BLOCK + tid;
+  static_assert(kThreads == E3_SAMPLE_BLOCK, "an entry a thread");
+  double r = 0.0, mass = 0.0;
+  if (i < w.V) r = exact_weight(w, kind, i, load_elem<DT>(w.z, i), kind == kDistribution ? load_elem<DT>(w.y, i) : 0.f, mass);
+  double sum = r;  // of the warp's entries up to this one
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const double up = __shfl_up_sync(kAll, sum, o);
+    if (lane >= o) sum += up;
+    mass += __shfl_xor_sync(kAll, mass, o);
+  }
+  __syncthreads();
+  if (lane == 31) {
+    sh[warp] = sum;
+    sh[kWarps + warp] = mass;
+  }
+  __syncthreads();
+  double total = 0.0;
+  mass = 0.0;
+#pragma unroll
+  for (int k = 0; k < kWarps; ++k) {
+    if (k < warp) sum += sh[k];
+    total += sh[k];
+    mass += sh[kWarps + k];
+  }
+  const double t = u * total, margin = exact || kind != kDistribution ? 0.0 : kZError * mass;
+  const bool near = i < w.V && margin > 0.0 && fabs(sum - t) <= margin;
+  int first = sum > t && r > 0.0 ? i : INT_MAX, last = r > 0.0 ? i : -1;
+  first = __reduce_min_sync(kAll, first);
+  last = __reduce_max_sync(kAll, last);
+  int *const ints = reinterpret_cast<int *>(sh);
+  const bool open = __syncthreads_or(near);  // (and the sums have been read)
+  if (lane == 0) {
+    ints[2 * warp] = first;
+    ints[2 * warp + 1] = last;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kWarps; ++k) {
+    first = min(first, ints[2 * k]);
+    last = max(last, ints[2 * k + 1]);
+  }
+  __syncthreads();
+  tok = first != INT_MAX ? first : last;
+  return !open && tok >= 0;
+}
+
+// Score of block b under p, but for the constant -ln Z (natural logarithms): ln of its sum plus its Gumbel variate.
+struct Score {
+  float y, off;  // value, bound on its error
+};
+__device__ __forceinline__ Score score_of_p(const float2 &s, double v, float R, float tau, int &bad) {
+  if (!usable_uniform(v)) bad = 1;
+  const float x = s.x > 0.f ? __fdiv_rn(fmaxf(s.y - R, -kFarBelow), tau) : -CUDART_INF_F, y = logf(s.x) + x + gumbel_of(v);
+  return Score{y, 1.2e-5f + 2e-6f * (fabsf(x) < 1e3f ? fabsf(x) : 1e3f)};
+}
+
+// Score of a block with weights p - q, with bounds, by a warp.
+template <int DT>
+__device__ __forceinline__ void score_block(const DrawRow &w, int b, float gumbel, float &lo, float &hi) {
   const int lane = threadIdx.x & 31, i0 = b * E3_SAMPLE_BLOCK + lane * 8;
   const Eight<DT> z = load_eight<DT>(w.z, w.V, i0);
   Eight<DT> y = z;
-  if (kind == kDistribution) y = load_eight<DT>(w.y, w.V, i0);
-  double r[8], mass = 0.0, sum = 0.0;
+  if (w.kind == kDistribution) y = load_eight<DT>(w.y, w.V, i0);
+  float r = 0.f, s = 0.f;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    double m = 0.0;
-    r[k] = i0 + k < w.V ? exact_weight(w, kind, i0 + k, entry<DT>(z, k), entry<DT>(y, k), m) : 0.0;
-    sum += r[k];
-    mass += m;
+  for (int h = 0; h < 8; ++h) {
+    const float zk = i0 + h < w.V ? entry<DT>(z, h) : -CUDART_INF_F;
+    const float e = ex2f(fmaf(zk - w.R, w.c, w.nz));
+    float q = 0.f;
+    if (w.kind == kDistribution) q = i0 + h < w.V ? ex2f(fmaf(entry<DT>(y, h) - w.y_d, w.cd, w.nq)) : 0.f;
+    if (w.kind == kOneHot && i0 + h == w.d) q = e;
+    r += fmaxf(e - q, 0.f);
+    s += e + (q <= 2.f ? q : 2.f);
   }
-  double before = sum;  // of the lanes up to this one, then of those before it
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const double up = __shfl_up_sync(kAll, before, o);
-    if (lane >= o) before += up;
-    mass += __shfl_xor_sync(kAll, mass, o);
+  for (int o = 16; o > 0; o >>= 1) {
+    r += __shfl_xor_sync(kAll, r, o);
+    s += __shfl_xor_sync(kAll, s, o);
   }
-  const double total = __shfl_sync(kAll, before, 31), t = u * total;
-  before = __shfl_up_sync(kAll, before, 1);
-  if (lane == 0) before = 0.0;
-  int first = INT_MAX, last = -1;
-  bool near = false;
-  const double margin = exact || kind != kDistribution ? 0.0 : kZError * mass;
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    before += r[k];
-    if (r[k] > 0.0) last = i0 + k;
-    if (before > t && r[k] > 0.0 && first == INT_MAX) first = i0 + k;
-    near |= i0 + k < w.V && fabs(before - t) <= margin && margin > 0.0;
-  }
-  first = __reduce_min_sync(kAll, first);
-  last = __reduce_max_sync(kAll, last);
-  tok = first != INT_MAX ? first : last;
-  return !__any_sync(kAll, near) && tok >= 0;
-}
-
-constexpr int kBlocksAhead[2] = {2, 4};  // blocks under way per warp: fp32, bf16
-
-// Scores of the blocks of this warp (every `step`-th from `from` on), with bounds on their errors.
-template <int DT>
-__device__ __forceinline__ Lead scan_blocks(const DrawRow &w, int blocks, const double *u, int from, int step) {
-  constexpr int kAhead = kBlocksAhead[DT];
-  const int lane = threadIdx.x & 31;
-  const float c = __fdiv_rn(kLog2e, w.tau), nz = -(float)(w.lnZ / kLn2);
-  const float cd = w.kind == kDistribution ? __fdiv_rn(kLog2e, w.tau_d) : 0.f, nq = w.kind == kDistribution ? (float)(w.lnq / kLn2) : 0.f;
-  Lead lead = no_lead();
-  float g = 0.f;
-  int n = 0;
-  for (int b0 = from; b0 < blocks; b0 += step * kAhead) {
-    Eight<DT> z[kAhead], y[kAhead];
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int b = b0 + k * step;
-      if (b < blocks) {
-        z[k] = load_eight<DT>(w.z, w.V, b * E3_SAMPLE_BLOCK + lane * 8);
-        if (w.kind == kDistribution) y[k] = load_eight<DT>(w.y, w.V, b * E3_SAMPLE_BLOCK + lane * 8);
-      }
-    }
-    if ((n & 31) == 0) {  // the variates of the next 32 blocks, one a lane
-      const int64_t b = b0 + (int64_t)lane * step;
-      const double ub = b < blocks ? u[b] : 0.5;
-      if (!usable_uniform(ub)) lead.bad = 1;
-      g = gumbel_of(ub);
-    }
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int b = b0 + k * step;
-      if (b >= blocks) break;
-      const int i0 = b * E3_SAMPLE_BLOCK + lane * 8;
-      float r = 0.f, s = 0.f;
-#pragma unroll
-      for (int h = 0; h < 8; ++h) {
-        const float zk = i0 + h < w.V ? entry<DT>(z[k], h) : -CUDART_INF_F;
-        const float e = ex2f(fmaf(zk - w.R, c, nz));
-        float q = 0.f;
-        if (w.kind == kDistribution) q = i0 + h < w.V ? ex2f(fmaf(entry<DT>(y[k], h) - w.y_d, cd, nq)) : 0.f;
-        if (w.kind == kOneHot && i0 + h == w.d) q = e;
-        r += fmaxf(e - q, 0.f);
-        s += e + (q <= 2.f ? q : 2.f);
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        r += __shfl_xor_sync(kAll, r, o);
-        s += __shfl_xor_sync(kAll, s, o);
-      }
-      const float gb = __shfl_sync(kAll, g, (n + k) & 31);
-      if (s > 0.f) {
-        const float off = s * (kSumError + kSumErrorPerBit * (fmaxf(-lg2f(s), 0.f) + 2.f * fabsf(nq))) + 1e-37f;
-        const float hi = logf(r + off) + gb, lo = r > off ? logf(r - off) + gb : -CUDART_INF_F;
-        insert(lead, lo - 6e-6f - 5e-7f * fabsf(lo), hi + 6e-6f + 5e-7f * fabsf(hi), b);
-      }
-    }
-    n += kAhead;
-  }
-  lead.bad = __any_sync(kAll, lead.bad != 0);
-  return lead;
+  const float off = s * (kSumError + kSumErrorPerBit * (fmaxf(-lg2f(s), 0.f) + 2.f * fabsf(w.nq))) + 1e-37f;
+  hi = logf(r + off) + gumbel;
+  lo = r > off ? logf(r - off) + gumbel : -CUDART_INF_F;
+  hi += 6e-6f + 5e-7f * fabsf(hi);
+  lo -= 6e-6f + 5e-7f * fabsf(lo);
 }
 
 struct Exact {
   double y;
   int b;
 };
-// The same in fp64; ties go to the lower block, blocks of weight 0 are left out.
+// Exact score of block b with the weights of `kind`, by a warp; false: weight 0.
 template <int DT>
-__device__ __noinline__ Exact scan_exact(const DrawRow &w, int kind, int blocks, const double *u, int from, int step) {
-  const int lane = threadIdx.x & 31;
-  Exact best = {0.0, INT_MAX};
-  for (int b = from; b < blocks; b += step) {
-    double r = 0.0, m;
-    for (int i = b * E3_SAMPLE_BLOCK + lane; i < w.V && i < (b + 1) * E3_SAMPLE_BLOCK; i += 32)
-      r += exact_weight(w, kind, i, load_elem<DT>(w.z, i), kind == kDistribution ? load_elem<DT>(w.y, i) : 0.f, m);
+__device__ __noinline__ bool exact_score_of(const DrawRow &w, int kind, int b, double u, double &y) {
+  const int lane = threadIdx.x & 31, i0 = b * E3_SAMPLE_BLOCK + lane * 8;
+  const Eight<DT> z = load_eight<DT>(w.z, w.V, i0);
+  Eight<DT> d = z;
+  if (kind == kDistribution) d = load_eight<DT>(w.y, w.V, i0);
+  double r = 0.0, m;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) r += __shfl_xor_sync(kAll, r, o);
-    if (r > 0.0) {
-      const double y = log(r) - log(-log(u[b]));
-      if (best.b == INT_MAX || y > best.y) best = {y, b};
-    }
-  }
-  return best;
+  for (int k = 0; k < 8; ++k)
+    if (i0 + k < w.V) r += exact_weight(w, kind, i0 + k, entry<DT>(z, k), entry<DT>(d, k), m);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) r += __shfl_xor_sync(kAll, r, o);
+  if (!(r > 0.0)) return false;
+  y = log(r) - log(-log(u));
+  return true;
 }
 __device__ __forceinline__ void merge(Exact &a, const Exact &o) {
   if (o.b != INT_MAX && (a.b == INT_MAX || o.y > a.y || (o.y == a.y && o.b < a.b))) a = o;
 }
+__device__ __forceinline__ Lead lead_of_warp(Lead l) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    Lead q;
+    q.lo = __shfl_xor_sync(kAll, l.lo, o);
+    q.hi1 = __shfl_xor_sync(kAll, l.hi1, o);
+    q.hi2 = __shfl_xor_sync(kAll, l.hi2, o);
+    q.lo_b = __shfl_xor_sync(kAll, l.lo_b, o);
+    q.hi_b = __shfl_xor_sync(kAll, l.hi_b, o);
+    q.bad = __shfl_xor_sync(kAll, l.bad, o);
+    merge(l, q);
+  }
+  return l;
+}
 
 struct DrawShared {
-  Lead lead[kWarps], cta;
-  Exact exact[kWarps], cta_exact;
-  double sum[kWarps], cta_sum;
-  int slow, again;
+  float score[kScoresKept];  // of the first blocks, under p: upper bounds
+  Lead lead[kWarps], all;
+  Exact exact[kWarps];
+  double sum[2 * kWarps];
+  int reached;  // score of p - q that some block reaches, encoded
 };
+// The CTA's lead from its warps', for every thread.
+__device__ __forceinline__ Lead lead_of_cta(const Lead &l, DrawShared &sh) {
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sh.lead[threadIdx.x >> 5] = l;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    const Lead all = lead_of_warp(threadIdx.x < kWarps ? sh.lead[threadIdx.x] : no_lead());
+    if (threadIdx.x == 0) sh.all = all;
+  }
+  __syncthreads();
+  return sh.all;
+}
 
+// A CTA draws for a sequence: a chain of dependent loads and small reductions, so all that depends on the position alone is fetched at once.
 template <int DT>
-__global__ void __launch_bounds__(kThreads, 3) draw_kernel(const __grid_constant__ VerifyParams p) {
+__global__ void __launch_bounds__(kThreads, 4) draw_kernel(const __grid_constant__ VerifyParams p) {
   __shared__ DrawShared sh;
-  const cg::cluster_group cluster = cg::this_cluster();
-  const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int64_t b = blockIdx.x / (unsigned)ctas;
+  const int tid = threadIdx.x, warp = __shfl_sync(kAll, tid >> 5, 0), lane = tid & 31;
+  const int64_t b = blockIdx.x;
+  if (tid == 0) sh.reached = enc_neg_inf();
   wait_for_stream_predecessor();
   const int len = length_of(p, b);
-  const int first = p.first[b], a = first < len ? first : len;
-  const int64_t r0 = b * (p.drafts + 1), r = r0 + a;
-  const VerifyRow rec = p.rows[r];
+  const int first = p.first[b];
   const float tau = p.temps[b];
-  if (rank == 0) {
-    for (int64_t j = tid; j <= p.drafts; j += kThreads) {
-      if (j == a) continue;
-      const VerifyRow q = j < a ? p.rows[r0 + j] : VerifyRow{};
-      p.out_tok[r0 + j] = j < a ? p.draft_tok[b * p.drafts + j] : -1;
-      if (p.out_logp != nullptr) p.out_logp[r0 + j] = j < a ? q.logp : 0.f;
-      if (p.out_ent != nullptr) p.out_ent[r0 + j] = j < a ? q.ent : 0.f;
+  int a = first < len ? first : len;
+  const int64_t r0 = b * (p.drafts + 1);
+  auto exact_total = [&](const char *row, float R) { return block_sum(exact_terms<DT>(row, p.V, R, tau, tid, kThreads), sh.sum); };
+  bool near = false;
+  for (int j = tid; j < a; j += kThreads) near |= p.rows[r0 + j].state == kNear;
+  VerifyRow rec = p.rows[r0 + a];
+  if (__syncthreads_or(near)) {  // positions that wait for a normaliser in fp64, in their order
+    for (int j = 0; j < a; ++j) {
+      const VerifyRow q = p.rows[r0 + j];
+      if (q.state != kNear) continue;
+      const char *const row = p.logits + (r0 + j) * p.row_bytes;
+      const double lnZ = log(exact_total(row, q.R));
+      const Draft d = draft_of<DT>(p, b, j);
+      const double lp = ((double)load_elem<DT>(row, d.tok) - (double)q.R) * (1.0 / (double)tau) - lnZ;
+      if (p.uniforms[b * p.u_stride + j] * exp(d.lnq) < exp(lp)) continue;
+      a = j;
+      rec = q;
+      rec.lnZ = lnZ;
+      rec.state = kRefused;
     }
-    if (tid == 0) p.out_kept[b] = a;
   }
-  auto write = [&](int tok, float logp, float ent) {  // by one thread
+  const int64_t r = r0 + a;
+  for (int64_t j = tid; j <= p.drafts; j += kThreads) {
+    if (j == a) continue;
+    const VerifyRow q = j < a ? p.rows[r0 + j] : VerifyRow{};
+    p.out_tok[r0 + j] = j < a ? p.draft_tok[b * p.drafts + j] : -1;
+    if (p.out_logp != nullptr) p.out_logp[r0 + j] = j < a ? q.logp : 0.f;
+    if (p.out_ent != nullptr) p.out_ent[r0 + j] = j < a ? q.ent : 0.f;
+  }
+  if (tid == 0) p.out_kept[b] = a;
+  auto write = [&](int tok, float logp, float ent) {
+    if (tid != 0) return;
     p.out_tok[r] = tok;
     if (p.out_logp != nullptr) p.out_logp[r] = logp;
     if (p.out_ent != nullptr) p.out_ent[r] = ent;
   };
-  if (rec.state == kInvalid) {
-    if (rank == 0 && tid == 0) write(-1, CUDART_NAN_F, CUDART_NAN_F);
-    return;
-  }
-  if (tau == 0.f) {
-    if (rank == 0 && tid == 0) write(rec.best, 0.f, 0.f);
-    return;
-  }
+  if (rec.state == kInvalid) return write(-1, CUDART_NAN_F, CUDART_NAN_F);
+  if (tau == 0.f) return write(rec.best, 0.f, 0.f);
   DrawRow w = {};
   w.z = p.logits + r * p.row_bytes;
   w.V = p.V; w.tau = tau; w.R = rec.R; w.lnZ = rec.lnZ; w.kind = kNoDraft; w.d = -1;
+  const double *const u = p.uniforms + b * p.u_stride + p.drafts;
+  const float2 *const sums = p.sums + r * p.blocks;
+  const double u_in = u[p.blocks];
+  // ---- scores under p: of the draw itself, or upper bounds (the first ones under way while the draft is looked up)
+  constexpr int kAhead = 4;
+  float2 sum[kAhead];
+  double v[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    const int i = tid + k * kThreads;
+    if (i < p.blocks) {
+      sum[k] = __ldcg(sums + i);
+      v[k] = u[i];
+    }
+  }
   if (a < len) {
     const Draft d = draft_of<DT>(p, b, a);
-    w.kind = d.kind; w.d = d.tok; w.y_d = d.y; w.tau_d = d.tau; w.lnq = d.lnq;
+    w.kind = d.kind; w.d = d.tok; w.y_d = d.y; w.lnq = d.lnq;
+    if (d.kind == kDistribution) {
+      w.beta_d = 1.0 / (double)d.tau; w.cd = __fdiv_rn(kLog2e, d.tau); w.nq = (float)(d.lnq * (1.0 / kLn2));
+    }
     w.y = p.draft_logits + (b * p.drafts + a) * p.draft_row_bytes;
   }
-  const double *const u = p.uniforms + b * p.u_stride + p.drafts;
-  const double u_in = u[p.blocks];
-  const int from = warp * ctas + rank, step = ctas * kWarps;
-  const Lead own = scan_blocks<DT>(w, p.blocks, u, from, step);
-  if (lane == 0) sh.lead[warp] = own;
-  __syncthreads();
-  if (tid == 0) {
-    Lead l = sh.lead[0];
-    for (int i = 1; i < kWarps; ++i) merge(l, sh.lead[i]);
-    sh.cta = l;
-  }
-  auto finish = [&](int tok) {  // by one thread
-    write(tok, (float)(((double)load_elem<DT>(w.z, tok) - (double)w.R) / (double)w.tau - w.lnZ), rec.ent);
+  Lead lead = no_lead();
+  auto enter = [&](int i, const float2 &s, double x) {
+    const Score y = score_of_p(s, x, w.R, w.tau, lead.bad);
+    if (i < kScoresKept) sh.score[i] = y.y + y.off;
+    insert(lead, y.y - y.off, y.y + y.off, i);
   };
-  cluster.sync();
-  if (rank == 0 && warp == 0) {
-    Lead l = lane < ctas ? *cluster.map_shared_rank(&sh.cta, lane) : no_lead();
 #pragma unroll
-    for (int o = 1; o < kClusterMost; o <<= 1) {
-      Lead q;
-      q.lo = __shfl_xor_sync(kAll, l.lo, o);
-      q.hi1 = __shfl_xor_sync(kAll, l.hi1, o);
-      q.hi2 = __shfl_xor_sync(kAll, l.hi2, o);
-      q.lo_b = __shfl_xor_sync(kAll, l.lo_b, o);
-      q.hi_b = __shfl_xor_sync(kAll, l.hi_b, o);
-      q.bad = __shfl_xor_sync(kAll, l.bad, o);
-      merge(l, q);
+  for (int k = 0; k < kAhead; ++k)
+    if (tid + k * kThreads < p.blocks) enter(tid + k * kThreads, sum[k], v[k]);
+  for (int i = tid + kAhead * kThreads; i < p.blocks; i += kThreads) enter(i, __ldcg(sums + i), u[i]);
+  w.beta = 1.0 / (double)tau; w.c = __fdiv_rn(kLog2e, tau); w.nz = -(float)(rec.lnZ * (1.0 / kLn2));
+  auto finish = [&](int tok) {
+    if (tok < 0) return write(-1, CUDART_NAN_F, CUDART_NAN_F);
+    if (tid == 0) write(tok, (float)(((double)load_elem<DT>(w.z, tok) - (double)w.R) * w.beta - w.lnZ), rec.ent);
+  };
+  lead = lead_of_cta(lead_of_warp(lead), sh);
+  if (lead.bad != 0 || !usable_uniform(u_in)) return write(-1, CUDART_NAN_F, CUDART_NAN_F);
+  float lnz = (float)w.lnZ;
+  const float reached_p = lead.lo - lnz;
+  if (w.kind != kNoDraft) {
+    // weights p - q: those blocks whose scores of p reach the best known score of p - q
+    int dummy = 0;
+    auto bound = [&](int i) {
+      if (i < kScoresKept) return sh.score[i];
+      const Score y = score_of_p(__ldcg(sums + i), u[i], w.R, w.tau, dummy);
+      return y.y + y.off;
+    };
+    Lead mine = no_lead();
+    float last = CUDART_INF_F;  // a warp takes its blocks in the order of their scores of p, highest first
+    int last_b = -1;
+    for (;;) {
+      float most = -CUDART_INF_F;
+      int at = INT_MAX;
+      for (int i = warp * 32 + lane; i < p.blocks; i += kThreads) {
+        const float y = bound(i);
+        if ((y < last || (y == last && i > last_b)) && y > most) {
+          most = y;
+          at = i;
+        }
+      }
+      const float top = dec_float(__reduce_max_sync(kAll, enc_float(most)));
+      const int i = __reduce_min_sync(kAll, most == top ? at : INT_MAX);
+      // (the two kinds of scores differ by ln Z)
+      if (i == INT_MAX || top - lnz + 4e-6f < dec_float(*(volatile int *)&sh.reached)) break;
+      float lo, hi;
+      score_block<DT>(w, i, gumbel_of(u[i]), lo, hi);
+      insert(mine, lo, hi, i);
+      if (lane == 0) atomicMax(&sh.reached, enc_float(lo));
+      __syncwarp();
+      last = top;
+      last_b = i;
     }
-    const bool bad = __shfl_sync(kAll, l.bad, 0) != 0 || !usable_uniform(u_in);
-    const int block = __shfl_sync(kAll, l.lo_b, 0);
-    const bool sure = __shfl_sync(kAll, l.lo > -CUDART_INF_F && l.hi_b == l.lo_b && l.lo > l.hi2, 0);
-    int tok = -1;
-    int slow = 0;
-    if (!bad) slow = !(sure && draw_in<DT>(w, w.kind, block, u_in, false, tok));
-    if (lane == 0 && bad) write(-1, CUDART_NAN_F, CUDART_NAN_F);
-    if (lane == 0 && !bad && !slow) finish(tok);
-    if (lane < ctas) *cluster.map_shared_rank(&sh.slow, lane) = slow;
+    lead = lead_of_cta(mine, sh);
   }
-  cluster.sync();
-  if (!sh.slow) return;
+  const bool sure = lead.lo > -CUDART_INF_F && lead.hi_b == lead.lo_b && lead.lo > lead.hi2;
+  int tok = -1;
+  if (sure && draw_in<DT>(w, w.kind, lead.lo_b, u_in, false, sh.sum, tok)) return finish(tok);
 
-  // ---- in fp64: the normaliser, then every block; where nothing is left of p - q, from p
-  {
-    const double part = block_sum(exact_terms<DT>(w.z, p.V, w.R, w.tau, rank * kThreads + tid, ctas * kThreads), sh.sum);
-    if (tid == 0) sh.cta_sum = part;
-    cluster.sync();
-    double total = 0.0;
-    for (int i = 0; i < ctas; ++i) total += *cluster.map_shared_rank(&sh.cta_sum, i);
-    w.lnZ = log(total);
+  // ---- the normaliser in fp64, and with it the blocks that the bounds did not exclude; where nothing is left of p - q, from p
+  w.lnZ = log(exact_total(w.z, w.R));
+  lnz = (float)w.lnZ;
+  if (sure) {
+    draw_in<DT>(w, w.kind, lead.lo_b, u_in, true, sh.sum, tok);
+    return finish(tok);
   }
   int kind = w.kind;
+  float floor = lead.lo;  // a score that some block reaches
   for (int round = 0; round < 2; ++round) {
-    const Exact e = scan_exact<DT>(w, kind, p.blocks, u, from, step);
+    Exact e = {0.0, INT_MAX};
+    for (int i0 = warp * 32; i0 < p.blocks; i0 += kThreads) {
+      int dummy = 0;
+      Score most = {-CUDART_INF_F, 0.f};
+      if (i0 + lane < p.blocks) most = score_of_p(__ldcg(sums + i0 + lane), u[i0 + lane], w.R, w.tau, dummy);
+      const float hi = most.y + most.off - lnz + 1e-5f;
+      uint32_t open = __ballot_sync(kAll, hi > -CUDART_INF_F && hi >= floor);
+      while (open != 0u) {
+        const int i = i0 + __ffs((int)open) - 1;
+        open &= open - 1u;
+        double y;
+        if (exact_score_of<DT>(w, kind, i, u[i], y)) merge(e, Exact{y, i});
+      }
+    }
     __syncthreads();
     if (lane == 0) sh.exact[warp] = e;
     __syncthreads();
-    if (tid == 0) {
-      Exact x = sh.exact[0];
-      for (int i = 1; i < kWarps; ++i) merge(x, sh.exact[i]);
-      sh.cta_exact = x;
+    e = sh.exact[0];
+    for (int i = 1; i < kWarps; ++i) merge(e, sh.exact[i]);
+    if (e.b != INT_MAX) {
+      draw_in<DT>(w, kind, e.b, u_in, true, sh.sum, tok);
+      return finish(tok);
     }
-    cluster.sync();
-    if (rank == 0 && warp == 0) {
-      Exact x = *cluster.map_shared_rank(&sh.cta_exact, 0);
-      for (int i = 1; i < ctas; ++i) merge(x, *cluster.map_shared_rank(&sh.cta_exact, i));
-      if (x.b != INT_MAX) {
-        int tok = -1;
-        draw_in<DT>(w, kind, x.b, u_in, true, tok);
-        if (lane == 0) finish(tok);
-      } else if (round == 1 && lane == 0) {
-        write(-1, CUDART_NAN_F, CUDART_NAN_F);
-      }
-      if (lane < ctas) *cluster.map_shared_rank(&sh.again, lane) = x.b == INT_MAX && round == 0;
-    }
-    cluster.sync();
-    if (!sh.again) return;
     kind = kNoDraft;
+    floor = reached_p - 1e-5f;
   }
+  write(-1, CUDART_NAN_F, CUDART_NAN_F);
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
 inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) != 0; }
 inline size_t up16(size_t b) { return (b + 15) / 16 * 16; }
 
-// Parts of a row: up to 64 KB each, smaller ones down to 8 KB where there are few rows, so that a call has about four CTAs an SM.
-constexpr int64_t kCtasWanted = 592;
-int part_entries(int64_t rows, int64_t V, int64_t esize, int &parts) {
-  const int64_t bytes = V * esize;
-  int64_t n = (bytes + 65535) / 65536;
-  if (rows * n < kCtasWanted) {
-    const int64_t more = kCtasWanted / rows, most = (bytes + 8191) / 8192;
-    if (n < (more < most ? more : most)) n = more < most ? more : most;
+// Parts of a row (blocks of one, and their number): what a CTA holds, or as much less as makes a call of few rows fill the SMs, down to a step a warp.
+constexpr int64_t kCtasHeld = kHeld * 148;
+int part_blocks(int64_t rows, int64_t blocks, int most, int least, int &parts) {
+  int64_t n = (blocks + most - 1) / most;
+  if (rows * n < kCtasHeld) {
+    const int64_t each = kCtasHeld / rows, finest = (blocks + least - 1) / least;
+    n = each < finest ? (each > n ? each : n) : (finest > n ? finest : n);
   }
-  if (n > kPartsMost) n = kPartsMost;
-  const int64_t part = ((V + n - 1) / n + 255) / 256 * 256;
-  parts = (int)((V + part - 1) / part);
+  int64_t part = (blocks + n - 1) / n;
+  while (rows * ((blocks + part - 1) / part) >= int64_t(1) << 31) part *= 2;
+  parts = (int)((blocks + part - 1) / part);
   return (int)part;
 }
 
 template <class... P, class... A>
-cudaError_t launch_behind(void (*kern)(P...), unsigned grid, int cluster, cudaStream_t stream, A &&...args) {
-  cudaLaunchAttribute attr[2];
+cudaError_t launch_behind(void (*kern)(P...), unsigned grid, int threads, size_t smem, cudaStream_t stream, A &&...args) {
+  cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)cluster;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cfg.attrs = attr;
-  cfg.numAttrs = cluster > 0 ? 2 : 1;
+  cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
 template <int DT>
-cudaError_t launch_verify(const VerifyParams &p, cudaStream_t stream) {
+cudaError_t launch_verify(VerifyParams &p, cudaStream_t stream) {
+  using F = Form<DT>;
+  constexpr int kSmemMost = kRowWarps * warp_bytes<DT>(F::kPartMost / kRowWarps);
+  static std::mutex lock;
+  static bool ready[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  {
+    std::lock_guard<std::mutex> hold(lock);
+    if (!ready[dev]) {
+      e = cudaFuncSetAttribute(verify_rows_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost);
+      if (e != cudaSuccess) return e;
+      ready[dev] = true;
+    }
+  }
   const int64_t rows = p.n_seq * (p.drafts + 1);
-  cudaError_t e = launch_behind(begin_kernel, (unsigned)(rows < 256 * 1024 ? (rows + 255) / 256 : 1024), 0, stream, p);
-  if (e == cudaSuccess) e = launch_behind(verify_rows_kernel<DT>, (unsigned)(rows * p.n_parts), 0, stream, p);
-  int ctas = kClusterMost;
-  while (ctas > 1 && (p.n_seq * ctas > kCtasWanted || p.blocks < ctas * kWarps)) ctas /= 2;
-  if (e == cudaSuccess) e = launch_behind(draw_kernel<DT>, (unsigned)(p.n_seq * ctas), ctas, stream, p);
+  p.part = part_blocks(rows, p.blocks, F::kPartMost, F::kStep * kRowWarps, p.n_parts);
+  const int round = p.part < F::kPartMost ? p.part : F::kPartMost;
+  e = launch_behind(begin_kernel, (unsigned)(rows < 256 * 1024 ? (rows + 255) / 256 : 1024), 256, 0, stream, p);
+  if (e == cudaSuccess)
+    e = launch_behind(verify_rows_kernel<DT>, (unsigned)(rows * p.n_parts), kRowThreads,
+                      (size_t)(kRowWarps * warp_bytes<DT>((round + kRowWarps - 1) / kRowWarps)), stream, p);
+  if (e == cudaSuccess) e = launch_behind(draw_kernel<DT>, (unsigned)p.n_seq, kThreads, 0, stream, p);
   return e;
 }
 
-size_t verify_layout(int64_t rows, size_t &arrived, size_t &records, size_t &parts) {
-  arrived = up16((size_t)rows * 4);
-  records = arrived + up16((size_t)rows * 4);
-  parts = records + (size_t)rows * sizeof(VerifyRow);
-  return parts + (size_t)rows * kPartsMost * sizeof(VerifyPart);
+struct Layout {
+  size_t arrived, records, parts, sums, bytes;
+};
+Layout layout(int64_t rows, int64_t blocks) {
+  Layout l;
+  l.arrived = up16((size_t)rows * 4);
+  l.records = l.arrived + up16((size_t)rows * 4);
+  l.parts = l.records + (size_t)rows * sizeof(VerifyRow);
+  l.sums = l.parts + (size_t)rows * (size_t)((blocks + 7) / 8) * sizeof(VerifyPart);  // (parts of at least eight blocks)
+  l.bytes = l.sums + (size_t)rows * (size_t)blocks * sizeof(float2);
+  return l;
 }
 
 }  // namespace
 
-size_t verify_workspace_bytes(int64_t rows) {
-  size_t a, r, p;
-  return verify_layout(rows < 0 ? 0 : rows, a, r, p);
+size_t verify_workspace_bytes(int64_t rows, int64_t V) {
+  return rows < 0 || V < 1 ? 0 : layout(rows, (V + E3_SAMPLE_BLOCK - 1) / E3_SAMPLE_BLOCK).bytes;
 }
 
 }  // namespace e3
@@ -829,9 +1100,9 @@ extern "C" e3_status e3_verify_drafts(const void *logits, e3_dtype dt, int64_t n
   using namespace e3;
   if (dt != E3_F32 && dt != E3_BF16) return E3_ERR_DTYPE;
   const int64_t most = int64_t(1) << 31;
-  if (n_seq < 0 || n_seq >= most || max_draft < 0 || max_draft >= most || V < 1 || V >= most - E3_SAMPLE_BLOCK || row_stride < V) return E3_ERR_INVALID_ARG;
+  if (n_seq < 0 || n_seq >= most || max_draft < 0 || max_draft >= most || V < 1 || V >= most - 65536 || row_stride < V) return E3_ERR_INVALID_ARG;
   const int64_t blocks = (V + E3_SAMPLE_BLOCK - 1) / E3_SAMPLE_BLOCK;
-  if (n_seq * (max_draft + 1) >= most / kPartsMost) return E3_ERR_INVALID_ARG;  // (the parts of all rows are one grid)
+  if (n_seq * (max_draft + 1) >= int64_t(1) << 26) return E3_ERR_INVALID_ARG;
   if (n_seq == 0) return E3_OK;
   if (!logits || !temps || !uniforms || uniform_stride < max_draft + blocks + 1 || !out_tok || !out_kept || (max_draft > 0 && !draft_tok))
     return E3_ERR_INVALID_ARG;
@@ -843,8 +1114,8 @@ extern "C" e3_status e3_verify_drafts(const void *logits, e3_dtype dt, int64_t n
       misaligned(out_logp, 4) || misaligned(out_ent, 4) || misaligned(workspace, 16))
     return E3_ERR_ALIGNMENT;
   const int64_t rows = n_seq * (max_draft + 1);
-  size_t arrived, records, parts;
-  if (!workspace || workspace_bytes < verify_layout(rows, arrived, records, parts)) return E3_ERR_WORKSPACE;
+  const Layout l = layout(rows, blocks);
+  if (!workspace || workspace_bytes < l.bytes) return E3_ERR_WORKSPACE;
   char *const ws = static_cast<char *>(workspace);
   VerifyParams p = {};
   p.logits = static_cast<const char *>(logits); p.draft_logits = static_cast<const char *>(draft_logits);
@@ -853,9 +1124,9 @@ extern "C" e3_status e3_verify_drafts(const void *logits, e3_dtype dt, int64_t n
   p.temps = temps; p.draft_temps = draft_temps; p.draft_logp = draft_logp; p.draft_tok = draft_tok; p.draft_len = draft_len;
   p.uniforms = uniforms; p.u_stride = uniform_stride;
   p.out_tok = out_tok; p.out_kept = out_kept; p.out_logp = out_logp; p.out_ent = out_ent;
-  p.first = reinterpret_cast<int32_t *>(ws); p.arrived = reinterpret_cast<int32_t *>(ws + arrived);
-  p.rows = reinterpret_cast<VerifyRow *>(ws + records); p.parts = reinterpret_cast<VerifyPart *>(ws + parts);
-  p.part = part_entries(rows, V, (int64_t)es, p.n_parts);
+  p.first = reinterpret_cast<int32_t *>(ws); p.arrived = reinterpret_cast<int32_t *>(ws + l.arrived);
+  p.rows = reinterpret_cast<VerifyRow *>(ws + l.records); p.parts = reinterpret_cast<VerifyPart *>(ws + l.parts);
+  p.sums = reinterpret_cast<float2 *>(ws + l.sums);
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
   const cudaError_t e = dt == E3_F32 ? launch_verify<0>(p, cs) : launch_verify<1>(p, cs);
   return e == cudaSuccess ? E3_OK : E3_ERR_CUDA;

@@ -570,7 +570,7 @@ PyObject *verify_drafts(PyObject *const *a) {
   const Output logp = checked_output(on, a[kLogp], "out_logp", truth(a[kWantLogp]), {n, k + 1}, at::kFloat);
   const Output ent = checked_output(on, a[kEnt], "out_ent", truth(a[kWantEnt]), {n, k + 1}, at::kFloat);
   const cudaStream_t stream = stream_of(a[kStream]);
-  const Scratch ws = checked_scratch(on, a[kWorkspace], e3_workspace_bytes(E3_CALL_VERIFY_DRAFTS, l.rows, 0, E3_F32), stream);
+  const Scratch ws = checked_scratch(on, a[kWorkspace], e3_workspace_bytes(E3_CALL_VERIFY_DRAFTS, l.rows, l.V, l.dt), stream);
   check("e3_verify_drafts", launch([&] {
           return e3_verify_drafts(l.data, l.dt, n, k, l.V, l.stride, pointer<float>(temps), pointer<int32_t>(drafts), pointer<int32_t>(len),
                                   draft_logits ? d.data : nullptr, d.stride, pointer<float>(draft_temps), pointer<float>(draft_logp),

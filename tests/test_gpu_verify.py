@@ -155,6 +155,12 @@ def test_longer_rows_and_many_sequences(e3, n, k, V):
         Batch(V, n, k, V, torch.bfloat16, model).check(e3)
 
 
+@pytest.mark.parametrize("dtype, V", [(torch.float32, 700003), (torch.bfloat16, 1500001)])
+def test_rows_longer_than_the_shared_memory_of_their_blocks(e3, dtype, V):
+    for model in (True, False):
+        Batch(V, 2, 1, V, dtype, model).check(e3)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_no_drafts_is_a_draw_from_the_target(e3, dtype):
     s = Batch(1, 6, 0, 5000, dtype, model=False)
@@ -303,7 +309,7 @@ def test_the_workspace_may_hold_anything(e3):
     s = Batch(12, 7, 3, 5000)
     want = s.call(e3)
     for fill in (0, 255, 1):
-        ws = torch.full((e3.e3_workspace_bytes(e3.E3_CALL_VERIFY_DRAFTS, 28),), fill, dtype=torch.uint8, device="cuda")
+        ws = torch.full((e3.e3_workspace_bytes(e3.E3_CALL_VERIFY_DRAFTS, 28, 5000),), fill, dtype=torch.uint8, device="cuda")
         assert all(torch.equal(x, y) for x, y in zip(s.call(e3, workspace=ws), want))
 
 

@@ -38,7 +38,7 @@ def test_verify_drafts_refuses(e3, change, status):
 
 
 def test_verify_workspace_grows_with_the_rows(e3):
-    size = [e3.e3_workspace_bytes(e3.E3_CALL_VERIFY_DRAFTS, n) for n in (0, 1, 5, 2560)]
+    size = [e3.e3_workspace_bytes(e3.E3_CALL_VERIFY_DRAFTS, n, 1000) for n in (0, 1, 5, 2560)]
     assert size == sorted(size) and size[-1] >= 2560 * 8
 
 
