@@ -1,11 +1,15 @@
 // The vocabulary's projection in 8 bits: logits[r, v] = sum_k sx[r, k] sw[v / 128, k] sum_{i in block k} x[r, i] w[v, i], x and w in e4m3.
 //
-// The table's rows are the tensor cores' M (128 of them, so that a tile has one table scale per block of 128 columns) and the hidden states'
-// rows are N, so that a call of a few rows streams the table through tiles of 128 x 16 and the logits of 32 neighbouring vocabulary entries
-// are written by the 32 lanes of a warp.  Persistent CTAs, one per SM: a producer thread keeps a ring of TMA copies (128 x 128 bytes of the
-// table and the tokens' 128 bytes each, swizzled) under way, one thread issues the tcgen05 products of a block into one of two accumulators in
-// tensor memory, a warp lays out the products of the scales, and one or two warpgroups take the block's sums from there, scale them and add them
-// up in fp32 registers.  8-bit products of 128 entries are added in 32 bits by the tensor cores, blocks in fp32 here; the logits are rounded once.
+// Two kernels of the same kind: persistent CTAs, one per SM; a producer thread keeps a ring of TMA copies (a block's 128 bytes of every row of both
+// operands, swizzled) under way, one thread issues the tcgen05 products of a block into one of two accumulators in tensor memory, and one or two
+// warpgroups take the block's sums from there, scale them and add them up in fp32 registers.  8-bit products of 128 entries are added in 32 bits by
+// the tensor cores, blocks in fp32 here; the logits are rounded once.
+//   - Up to 64 rows: the table's rows are the tensor cores' M (128 of them: one table scale per tile and block), the hidden states' rows their N, so
+//     that the table streams through tiles of 128 x 16, 32 or 64; bound by reading the table.  A lane has a vocabulary entry, the rows' scales come from
+//     shared memory.
+//   - More rows: 128 of the hidden states' rows are M and 256 vocabulary entries N.  A lane has a row, so that its scale is one register and the
+//     sums cost one multiply-add per entry and block and nothing else (with the other form's scales, four bytes per entry and block from shared
+//     memory, a block of 128 x 256 x 128 took 2,200 cycles, the products 512).
 //
 // Every wait is bounded: one that runs out marks the call's status word, and the CTA's unfinished logits read NaN.
 #include "e3_rows_device.cuh"
@@ -33,17 +37,17 @@ struct ProjectParams {
   int64_t out_stride;
   int32_t *status;
   int rows, V, blocks;  // blocks: of 128 columns
-  int row_tiles;
-  int64_t tiles;        // row tiles run fastest: neighbours share the table's rows in L2
+  uint32_t row_tiles;
+  int vectors;          // the logits' rows begin on 16-byte boundaries
+  uint32_t tiles;       // row tiles run fastest: neighbours share the table's rows in L2
   u64 wait_ns;
 };
 
 // NT: rows of the hidden states in a tile (N of the products).
 template <int NT>
 struct Plan {
-  static constexpr int kGroups = NT > 128 ? 2 : 1;           // warpgroups that take sums
-  static constexpr int kSumWarps = 4 * kGroups;
-  static constexpr int kCols = NT / kGroups;                 // columns of a thread
+  static constexpr int kSumWarps = 4;
+  static constexpr int kCols = NT;                           // columns of a thread
   static constexpr int kThreads = (kSumWarps + 3) * 32;      // and a producer, an issuer, a warp for the scales
   static constexpr int kStageBytes = (kTileV + NT) * kTileK;
   static constexpr int kStages = kSmemMost / kStageBytes < 12 ? kSmemMost / kStageBytes : 12;
@@ -65,17 +69,33 @@ struct __align__(16) Shared {
 __device__ __forceinline__ void mbar_arrive(u64 *b) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(b)) : "memory");
 }
-// Waits for a phase; false after the limit, or once another thread of the CTA has given up.
-__device__ __forceinline__ bool wait_for(u64 *b, uint32_t parity, int *gave_up, u64 limit) {
-  if (mbar_try_wait(b, parity)) return true;
-  const u64 t0 = global_ns();
-  for (uint32_t it = 1;; ++it) {
+// Waits for a phase; false after the limit, or once another thread of the CTA has given up.  (The global timer is slow to read: not before some polls.)
+__device__ __noinline__ bool wait_longer(u64 *b, uint32_t parity, int *gave_up, u64 limit) {
+  u64 t0 = 0;
+  for (uint32_t it = 0;; ++it) {
     if (mbar_try_wait(b, parity)) return true;
-    if ((it & 31u) == 0u && (*(volatile int *)gave_up != 0 || global_ns() - t0 > limit)) {
-      *(volatile int *)gave_up = 1;
-      return false;
+    if ((it & 63u) == 63u) {
+      const u64 now = global_ns();
+      if (t0 == 0) t0 = now;
+      if (*(volatile int *)gave_up != 0 || now - t0 > limit) {
+        *(volatile int *)gave_up = 1;
+        return false;
+      }
     }
   }
+}
+__device__ __forceinline__ bool wait_for(u64 *b, uint32_t parity, int *gave_up, u64 limit) {
+  return mbar_try_wait(b, parity) || wait_longer(b, parity, gave_up, limit);
+}
+// One lane of the warp, always the same.  Loops whose copies and products one lane issues are run by the whole warp: their operands sit in uniform
+// registers, and with a lane's own branch around the loop the compiler has to bring each there by a loop over the lanes (800 cycles a block).
+__device__ __forceinline__ bool elected() {
+  uint32_t is;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+  return is != 0;
+}
+__device__ __forceinline__ bool wait_as_warp(u64 *b, uint32_t parity, int *gave_up, u64 limit) {
+  return __all_sync(0xffffffffu, wait_for(b, parity, gave_up, limit));
 }
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y, u64 *bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
@@ -153,28 +173,30 @@ __global__ void __launch_bounds__(Plan<NT>::kThreads, 1)
   }
   __syncthreads();
   fence_after();
-  const uint32_t tmem = sh.tmem;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
   if (warp == L::kSumWarps) {
     // ---- producer
-    if (lane == 0) {
+    {
       uint32_t n = 0;
       bool on = true;
-      for (int64_t tile = blockIdx.x; tile < p.tiles && on; tile += gridDim.x) {
+      for (uint32_t tile = blockIdx.x; tile < p.tiles && on; tile += gridDim.x) {
         const int tv = (int)(tile / p.row_tiles) * kTileV, tr = (int)(tile % p.row_tiles) * NT;
         for (int k = 0; k < p.blocks && on; ++k, ++n) {
           const uint32_t s = n % L::kStages, round = n / L::kStages;
-          on = wait_for(&sh.empty[s], (round & 1u) ^ 1u, &sh.gave_up, p.wait_ns);
+          on = wait_as_warp(&sh.empty[s], (round & 1u) ^ 1u, &sh.gave_up, p.wait_ns);
           if (!on) break;
           const uint32_t at = ring + s * L::kStageBytes;
-          mbar_arrive_expect(&sh.full[s], L::kStageBytes);
-          tma_load(at, &w_map, k * kTileK, tv, &sh.full[s]);
-          tma_load(at + kTileV * kTileK, &x_map, k * kTileK, tr, &sh.full[s]);
+          if (elected()) {
+            mbar_arrive_expect(&sh.full[s], L::kStageBytes);
+            tma_load(at, &w_map, k * kTileK, tv, &sh.full[s]);
+            tma_load(at + kTileV * kTileK, &x_map, k * kTileK, tr, &sh.full[s]);
+          }
         }
       }
-      if (!on) {  // given up: the copies under way still land in this CTA's memory
+      if (!on && lane == 0) {  // given up: the copies under way still land in this CTA's memory
         for (uint32_t m = n > L::kStages ? n - L::kStages : 0; m < n; ++m) {
           const u64 t0 = global_ns();
           while (!mbar_try_wait(&sh.full[m % L::kStages], (m / L::kStages) & 1u) && global_ns() - t0 < p.wait_ns) {
@@ -184,29 +206,32 @@ __global__ void __launch_bounds__(Plan<NT>::kThreads, 1)
     }
   } else if (warp == L::kSumWarps + 1) {
     // ---- issuer of the products
-    if (lane == 0) {
+    {
       // fp32 sums of e4m3 x e4m3, both operands along their rows
       constexpr uint32_t kForm = 1u << 4 | (uint32_t)(NT >> 3) << 17 | (uint32_t)(kTileV >> 4) << 24;
       uint32_t n = 0;
       bool on = true;
-      for (int64_t tile = blockIdx.x; tile < p.tiles && on; tile += gridDim.x) {
+      for (uint32_t tile = blockIdx.x; tile < p.tiles && on; tile += gridDim.x) {
         for (int k = 0; k < p.blocks && on; ++k, ++n) {
           const uint32_t s = n % L::kStages, round = n / L::kStages, half = n & 1u;
-          on = wait_for(&sh.sum_empty[half], ((n >> 1) & 1u) ^ 1u, &sh.gave_up, p.wait_ns) &&
-               wait_for(&sh.full[s], round & 1u, &sh.gave_up, p.wait_ns);
+          on = wait_as_warp(&sh.sum_empty[half], ((n >> 1) & 1u) ^ 1u, &sh.gave_up, p.wait_ns) &&
+               wait_as_warp(&sh.full[s], round & 1u, &sh.gave_up, p.wait_ns);
           if (!on) break;
           fence_after();
           const uint32_t at = ring + s * L::kStageBytes;
           const u64 a = operand(at), b = operand(at + kTileV * kTileK);
+          if (elected()) {
 #pragma unroll
-          for (int i = 0; i < kTileK / 32; ++i)  // 32 bytes of every row at a time
-            multiply(tmem + half * NT, a + (u64)(2 * i), b + (u64)(2 * i), kForm, i > 0);
-          commit(&sh.empty[s]);
-          commit(&sh.sum_full[half]);
+            for (int i = 0; i < kTileK / 32; ++i)  // 32 bytes of every row at a time
+              multiply(tmem + half * NT, a + (u64)(2 * i), b + (u64)(2 * i), kForm, i > 0);
+            commit(&sh.empty[s]);
+            commit(&sh.sum_full[half]);
+          }
         }
       }
       // products under way (there are some if the CTA has given up) write the tensor memory, and their signals its shared memory
-      commit(&sh.drained);
+      if (elected()) commit(&sh.drained);
+      __syncwarp();
       const u64 t0 = global_ns();
       while (!mbar_try_wait(&sh.drained, 0) && global_ns() - t0 < p.wait_ns) {
       }
@@ -216,7 +241,7 @@ __global__ void __launch_bounds__(Plan<NT>::kThreads, 1)
     constexpr int kEach = (NT + 31) / 32;
     uint32_t n = 0;
     bool on = true;
-    for (int64_t tile = blockIdx.x; tile < p.tiles && on; tile += gridDim.x) {
+    for (uint32_t tile = blockIdx.x; tile < p.tiles && on; tile += gridDim.x) {
       const int64_t tv = tile / p.row_tiles;
       const int tr = (int)(tile % p.row_tiles) * NT;
       for (int k0 = 0; k0 < p.blocks && on; k0 += kScaleGroup) {
@@ -247,13 +272,12 @@ __global__ void __launch_bounds__(Plan<NT>::kThreads, 1)
   } else {
     // ---- sums: a thread has one vocabulary entry and kCols rows
     constexpr int kCols = L::kCols;
-    const int group = warp >> 2;
-    const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + group * kCols;  // (lane 32 (warp mod 4) of the tensor memory)
+    const uint32_t from = tmem + ((uint32_t)warp << 21);  // (lane 32 warp of the tensor memory)
     uint32_t n = 0;
     bool on = true;
-    for (int64_t tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
-      const int64_t v = (tile / p.row_tiles) * kTileV + (warp & 3) * 32 + lane;
-      const int r0 = (int)(tile % p.row_tiles) * NT + group * kCols;
+    for (uint32_t tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
+      const int64_t v = (int64_t)(tile / p.row_tiles) * kTileV + warp * 32 + lane;
+      const int r0 = (int)(tile % p.row_tiles) * NT;
       f2 sum[kCols / 2];
 #pragma unroll
       for (int i = 0; i < kCols / 2; ++i) sum[i] = pack2f(0.f, 0.f);
@@ -263,7 +287,7 @@ __global__ void __launch_bounds__(Plan<NT>::kThreads, 1)
                                          wait_for(&sh.sum_full[half], (n >> 1) & 1u, &sh.gave_up, p.wait_ns));
         if (!on) break;
         fence_after();
-        const uint32_t scale = smem_addr(&sh.scale[s][group * kCols]);
+        const uint32_t scale = smem_addr(&sh.scale[s][0]);
         float t[2][16];
         tmem_load16(from + half * NT, t[0]);
 #pragma unroll
@@ -303,6 +327,311 @@ __global__ void __launch_bounds__(Plan<NT>::kThreads, 1)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::kTmemCols));
   }
 }
+
+// ---- many rows -----------------------------------------------------------------------------------------------------
+namespace wide {
+
+// A tile has 128 rows and 256 vocabulary entries.  The issuing warp needs about 500 cycles a block however wide its products are (two waits, four
+// products, a signal), so they are as wide as they can be: 512 cycles.
+constexpr int kM = 128, kN = 256;
+constexpr int kBuffers = 2;
+constexpr int kCols = 128;             // columns of a thread
+constexpr int kAhead = 2;              // blocks whose scales are fetched together
+constexpr int kSumWarps = 4 * kN / kCols;
+constexpr int kThreads = (kSumWarps + 2) * 32;
+constexpr int kStageBytes = (kM + kN) * kTileK;
+constexpr int kStages = 4;
+// Finished logits go through shared memory, 64 bytes of each of a warp's 32 rows at a time, so that they leave in pieces of rows.
+constexpr int kPieceBytes = 64, kPieces = 32 * kPieceBytes;
+constexpr size_t kSmem = (size_t)kStages * kStageBytes + kSumWarps * 2 * kPieces + 1024;
+static_assert(kSmem + 512 <= 227 * 1024, "shared memory");
+
+// Where 16 bytes of a row lie: spread so that neither eight rows' first parts nor two rows' four parts meet in a bank.
+__device__ __forceinline__ uint32_t piece_at(int row, int part) { return (uint32_t)(row * kPieceBytes + ((part ^ ((row >> 1) & 3)) << 4)); }
+
+struct Shared {
+  u64 full[kStages], empty[kStages];
+  u64 sum_full[kBuffers], sum_empty[kBuffers];
+  u64 drained;
+  uint32_t tmem;
+  int gave_up;
+};
+
+// 16 columns of the tensor memory; they may be read behind tmem_wait.
+__device__ __forceinline__ void tmem_begin16(uint32_t addr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// (volatile: stays behind the wait.  Operands that pass through the wait, or leave one block with it, cost a move each.)
+__device__ __forceinline__ void add_scaled(u64 &sum, uint32_t lo, uint32_t hi, u64 scale) {
+  asm volatile("{ .reg .b64 v; mov.b64 v, {%1, %2}; fma.rn.f32x2 %0, v, %3, %0; }" : "+l"(sum) : "r"(lo), "r"(hi), "l"(scale));
+}
+__device__ __forceinline__ f2 pair_of(u64 v) { return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))); }
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint32_t bf16_pair(f2 v) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
+  return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+template <int OUT>
+__global__ void __launch_bounds__(kThreads, 1)
+    project_rows_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ ProjectParams p) {
+  extern __shared__ unsigned char dyn[];
+  __shared__ Shared sh;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+  const uint32_t ring = (smem_addr(dyn) + 1023u) & ~1023u;
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(&sh.full[i], 1);
+      mbar_init(&sh.empty[i], 1);
+    }
+    for (int i = 0; i < kBuffers; ++i) {
+      mbar_init(&sh.sum_full[i], 1);
+      mbar_init(&sh.sum_empty[i], kSumWarps);
+    }
+    mbar_init(&sh.drained, 1);
+    sh.gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_smem();
+  }
+  if (warp == kSumWarps + 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&sh.tmem)), "r"(kBuffers * kN) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    fence_before();
+  }
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  if (warp == kSumWarps) {
+    // ---- producer
+    {
+      uint32_t n = 0;
+      bool on = true;
+      for (uint32_t tile = blockIdx.x; tile < p.tiles && on; tile += gridDim.x) {
+        const int tv = (int)(tile / p.row_tiles) * kN, tr = (int)(tile % p.row_tiles) * kM;
+        for (int k = 0; k < p.blocks && on; ++k, ++n) {
+          const uint32_t s = n % kStages, round = n / kStages;
+          on = wait_as_warp(&sh.empty[s], (round & 1u) ^ 1u, &sh.gave_up, p.wait_ns);
+          if (!on) break;
+          const uint32_t at = ring + s * kStageBytes;
+          if (elected()) {
+            mbar_arrive_expect(&sh.full[s], kStageBytes);
+            tma_load(at, &x_map, k * kTileK, tr, &sh.full[s]);
+            tma_load(at + kM * kTileK, &w_map, k * kTileK, tv, &sh.full[s]);
+          }
+        }
+      }
+      if (!on && lane == 0) {  // given up: the copies under way still land in this CTA's memory
+        for (uint32_t m = n > kStages ? n - kStages : 0; m < n; ++m) {
+          const u64 t0 = global_ns();
+          while (!mbar_try_wait(&sh.full[m % kStages], (m / kStages) & 1u) && global_ns() - t0 < p.wait_ns) {
+          }
+        }
+      }
+    }
+  } else if (warp == kSumWarps + 1) {
+    // ---- issuer of the products
+    {
+      constexpr uint32_t kForm = 1u << 4 | (uint32_t)(kN >> 3) << 17 | (uint32_t)(kM >> 4) << 24;
+      uint32_t n = 0;
+      bool on = true;
+      for (uint32_t tile = blockIdx.x; tile < p.tiles && on; tile += gridDim.x) {
+        for (int k = 0; k < p.blocks && on; ++k, ++n) {
+          const uint32_t s = n % kStages, round = n / kStages, half = n % kBuffers;
+          // both waits at once, as a rule there is nothing to wait for
+          const bool here = mbar_try_wait(&sh.sum_empty[half], ((n / kBuffers) & 1u) ^ 1u), there = mbar_try_wait(&sh.full[s], round & 1u);
+          if (!__all_sync(0xffffffffu, here && there))
+            on = wait_as_warp(&sh.sum_empty[half], ((n / kBuffers) & 1u) ^ 1u, &sh.gave_up, p.wait_ns) &&
+                 wait_as_warp(&sh.full[s], round & 1u, &sh.gave_up, p.wait_ns);
+          if (!on) break;
+          fence_after();
+          const uint32_t at = ring + s * kStageBytes;
+          const u64 a = operand(at), b = operand(at + kM * kTileK);
+          if (elected()) {
+#pragma unroll
+            for (int i = 0; i < kTileK / 32; ++i) multiply(tmem + half * kN, a + (u64)(2 * i), b + (u64)(2 * i), kForm, i > 0);
+            commit(&sh.sum_full[half]);
+          }
+        }
+      }
+      // products under way (there are some if the CTA has given up) write the tensor memory, and their signals its shared memory
+      if (elected()) commit(&sh.drained);
+      __syncwarp();
+      const u64 t0 = global_ns();
+      while (!mbar_try_wait(&sh.drained, 0) && global_ns() - t0 < p.wait_ns) {
+      }
+    }
+  } else {
+    // ---- sums: a thread has one row and kCols vocabulary entries
+    constexpr int kEsize = OUT == 0 ? 4 : 2, kPieceCols = kPieceBytes / kEsize;
+    const int group = warp >> 2, row_of_warp = (warp & 3) * 32;
+    const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + group * kCols;  // (lane 32 (warp mod 4) of the tensor memory)
+    const uint32_t piece = ring + kStages * kStageBytes + warp * 2 * kPieces;
+    uint32_t n = 0;
+    bool on = true;
+    // scales of four blocks ahead, the next tile's first ones too: the row's, and the table's for these entries (multiplied when they are needed, or
+    // the loads would be waited for here)
+    float next_x[kAhead], next_w[kAhead];
+    const float *sx, *sw, *next_sx, *next_sw;
+    auto point_at = [&](uint32_t tile, const float *&sx, const float *&sw) {
+      const uint32_t tv = tile / p.row_tiles;
+      const int64_t r = (int64_t)(tile - tv * p.row_tiles) * kM + row_of_warp + lane;
+      sx = p.x_scale + (r < p.rows ? r : 0) * p.x_scale_stride;
+      const int64_t block = ((int64_t)tv * kN + group * kCols) / E3_SCALE_BLOCK;  // (a tile may reach past the last)
+      sw = p.w_scale + (block * E3_SCALE_BLOCK < p.V ? block : 0) * p.w_scale_stride;
+    };
+    auto fetch = [&](int k0) {
+      if (k0 + kAhead <= p.blocks) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          next_x[k] = sx[k0 + k];
+          next_w[k] = sw[k0 + k];
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          next_x[k] = sx[k0 + k < p.blocks ? k0 + k : 0];
+          next_w[k] = sw[k0 + k < p.blocks ? k0 + k : 0];
+        }
+      }
+    };
+    static_assert(E3_SCALE_BLOCK % kCols == 0, "one scale of the table a thread and block");
+    point_at(blockIdx.x, next_sx, next_sw);
+    sx = next_sx;
+    sw = next_sw;
+    fetch(0);
+    for (uint32_t tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
+      const int64_t v0 = (int64_t)(tile / p.row_tiles) * kN + group * kCols;
+      const int64_t r0 = (int64_t)(tile % p.row_tiles) * kM + row_of_warp;
+      // the next tile's scales are on their way while this one is summed: from memory they take as long as three blocks
+      const bool more = tile + gridDim.x < p.tiles;
+      if (more) {
+        point_at(tile + gridDim.x, next_sx, next_sw);
+        for (int k = 0; k < p.blocks; k += 32) {
+          asm volatile("prefetch.global.L1 [%0];" ::"l"(next_sx + k));
+          asm volatile("prefetch.global.L1 [%0];" ::"l"(next_sw + k));
+        }
+      }
+      u64 sum[kCols / 2];
+#pragma unroll
+      for (int i = 0; i < kCols / 2; ++i) sum[i] = 0ull;
+      float scale[kAhead];
+#pragma unroll 1
+      for (int k = 0; k < p.blocks && on; ++k, ++n) {
+        if ((k & (kAhead - 1)) == 0) {
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) scale[i] = next_x[i] * next_w[i];
+          if (k + kAhead < p.blocks) {
+            fetch(k + kAhead);
+          } else if (more) {
+            sx = next_sx;
+            sw = next_sw;
+            fetch(0);
+          }
+        }
+        const uint32_t bits = __float_as_uint(scale[0]);
+        const u64 c2 = (u64)bits << 32 | bits;
+        scale[0] = scale[1];
+        const uint32_t half = n % kBuffers;
+        on = wait_as_warp(&sh.sum_full[half], (n / kBuffers) & 1u, &sh.gave_up, p.wait_ns);
+        if (!on) break;
+        // (the products have read their operands too)
+        if (warp == 0 && lane == 0) mbar_arrive(&sh.empty[n % kStages]);
+        fence_after();
+#pragma unroll
+        for (int q = 0; q < kCols / 16; ++q) {
+          uint32_t t[16];
+          tmem_begin16(from + half * kN + q * 16, t);
+          tmem_wait();
+          if (q + 1 == kCols / 16) {
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.sum_empty[half]);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) add_scaled(sum[q * 8 + i], t[2 * i], t[2 * i + 1], c2);
+        }
+      }
+      // ---- the tile's logits, two pieces at a time
+      if (!on) {
+#pragma unroll
+        for (int i = 0; i < kCols / 2; ++i) sum[i] = 0x7FC000007FC00000ull;
+      }
+      const int left = (int)(p.rows - r0 < 32 ? p.rows - r0 : 32);  // rows of this warp
+      char *const to = static_cast<char *>(p.out) + (r0 * p.out_stride + v0) * kEsize;
+      const int64_t row_bytes = p.out_stride * kEsize;
+      char *const mine = to + (lane >> 2) * row_bytes + (lane & 3) * 16;  // of this lane's 16 bytes of the first eight rows
+      const bool whole = p.vectors != 0 && left == 32 && v0 + kCols <= p.V;
+#pragma unroll
+      for (int q = 0; q < kCols / kPieceCols; q += 2) {
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t w[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+              if (OUT == 1) {
+                w[h] = bf16_pair(pair_of(sum[(q + j) * 16 + i * 4 + h]));
+              } else {
+                const f2 x = pair_of(sum[(q + j) * 8 + i * 2 + (h >> 1)]);
+                w[h] = __float_as_uint((h & 1) != 0 ? x.y : x.x);
+              }
+            }
+            sts128(piece + (uint32_t)(j * kPieces) + piece_at(lane, i), w[0], w[1], w[2], w[3]);
+          }
+        }
+        __syncwarp();
+        if (whole) {
+          uint4 x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = lds128(piece + (uint32_t)((i >> 2) * kPieces) + piece_at((i & 3) * 8 + (lane >> 2), lane & 3));
+#pragma unroll
+          for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4 *>(mine + (i & 3) * 8 * row_bytes + (q + (i >> 2)) * kPieceBytes) = x[i];
+        } else {
+          const int col = lane % kPieceCols, step = 32 / kPieceCols;
+#pragma unroll 1
+          for (int j = 0; j < 2; ++j) {
+            if (v0 + (q + j) * kPieceCols + col >= p.V) continue;
+#pragma unroll 4
+            for (int rr = lane / kPieceCols; rr < left; rr += step) {
+              const uint32_t at = piece + (uint32_t)(j * kPieces) + piece_at(rr, col * kEsize >> 4) + (uint32_t)(col * kEsize & 15);
+              char *const there = to + rr * row_bytes + ((q + j) * kPieceCols + col) * kEsize;
+              if (OUT == 0) {
+                *reinterpret_cast<float *>(there) = lds_elem<0>(at);
+              } else {
+                unsigned short h;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at));
+                *reinterpret_cast<unsigned short *>(there) = h;
+              }
+            }
+          }
+        }
+      }
+    }
+    if (!on && lane == 0 && p.status != nullptr) atomicOr(p.status, kStatusTimeout);
+  }
+  fence_before();
+  __syncthreads();
+  if (warp == kSumWarps + 1) {
+    __syncwarp();
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kBuffers * kN));
+  }
+}
+
+}  // namespace wide
 
 // ---- host side -----------------------------------------------------------------------------------------------------
 inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) != 0; }
@@ -370,13 +699,15 @@ cudaError_t launch(Call &c, cudaStream_t stream) {
       !make_map(encode, &x_map, c.x, c.p.rows, c.D, c.x_stride, NT))
     return cudaErrorInvalidValue;
   c.p.row_tiles = (c.p.rows + NT - 1) / NT;
-  c.p.tiles = (int64_t)((c.p.V + kTileV - 1) / kTileV) * c.p.row_tiles;
+  const int64_t tiles = (int64_t)((c.p.V + kTileV - 1) / kTileV) * c.p.row_tiles;
+  if (tiles >= (int64_t)1 << 31) return cudaErrorInvalidValue;
+  c.p.tiles = (uint32_t)tiles;
   c.p.wait_ns = kDefaultWaitNs;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(c.p.tiles < sms ? c.p.tiles : sms));
+  cfg.gridDim = dim3((unsigned)(tiles < sms ? tiles : sms));
   cfg.blockDim = dim3(L::kThreads);
   cfg.dynamicSmemBytes = L::kSmem;
   cfg.stream = stream;
@@ -386,12 +717,50 @@ cudaError_t launch(Call &c, cudaStream_t stream) {
 }
 
 template <int OUT>
+cudaError_t launch_wide(Call &c, cudaStream_t stream) {
+  static std::mutex lock;
+  static bool ready[64];
+  auto kern = wide::project_rows_kernel<OUT>;
+  int dev = 0;
+  const int sms = sm_count(dev);
+  if (sms == 0) return cudaErrorInvalidDevice;
+  {
+    std::lock_guard<std::mutex> hold(lock);
+    if (!ready[dev]) {
+      const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)wide::kSmem);
+      if (e != cudaSuccess) return e;
+      ready[dev] = true;
+    }
+  }
+  const Encode encode = encode_function();
+  CUtensorMap w_map, x_map;
+  if (encode == nullptr || !make_map(encode, &w_map, c.w, c.p.V, c.D, c.w_stride, wide::kN) ||
+      !make_map(encode, &x_map, c.x, c.p.rows, c.D, c.x_stride, wide::kM))
+    return cudaErrorInvalidValue;
+  c.p.row_tiles = (c.p.rows + wide::kM - 1) / wide::kM;
+  const int64_t tiles = (int64_t)((c.p.V + wide::kN - 1) / wide::kN) * c.p.row_tiles;
+  if (tiles >= (int64_t)1 << 31) return cudaErrorInvalidValue;
+  c.p.tiles = (uint32_t)tiles;
+  c.p.wait_ns = kDefaultWaitNs;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles < sms ? tiles : sms));
+  cfg.blockDim = dim3(wide::kThreads);
+  cfg.dynamicSmemBytes = wide::kSmem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, x_map, w_map, c.p);
+}
+
+template <int OUT>
 cudaError_t launch_sized(Call &c, cudaStream_t stream) {
   if (c.p.rows <= 16) return launch<16, OUT>(c, stream);
   if (c.p.rows <= 32) return launch<32, OUT>(c, stream);
   if (c.p.rows <= 64) return launch<64, OUT>(c, stream);
-  if (c.p.rows <= 128) return launch<128, OUT>(c, stream);
-  return launch<256, OUT>(c, stream);
+  return launch_wide<OUT>(c, stream);
 }
 
 }  // namespace
@@ -417,6 +786,7 @@ extern "C" e3_status e3_project_vocab(const uint8_t *x, const float *x_scale, in
   c.p.x_scale = x_scale; c.p.w_scale = w_scale; c.p.x_scale_stride = x_scale_stride; c.p.w_scale_stride = w_scale_stride;
   c.p.out = logits; c.p.out_stride = row_stride; c.p.status = out_status;
   c.p.rows = (int)rows; c.p.V = (int)V; c.p.blocks = (int)blocks;
+  c.p.vectors = !misaligned(logits, 16) && row_stride * (dt == E3_F32 ? 4 : 2) % 16 == 0;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
   const cudaError_t e = dt == E3_F32 ? launch_sized<0>(c, cs) : launch_sized<1>(c, cs);
   return e == cudaSuccess ? E3_OK : E3_ERR_CUDA;
