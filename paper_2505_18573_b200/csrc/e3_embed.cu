@@ -19,8 +19,8 @@ constexpr int kDigitsMost = 1024;    // buckets of the upper digit
 constexpr int kLowMost = 12;         // bits of the lower digit
 constexpr int kTilesMost = 512;
 constexpr int64_t kVMost = int64_t(kDigitsMost) << kLowMost;
-constexpr int64_t kDMost = int64_t(1) << 24;  // (columns are blockIdx.y)
-static_assert(kDMost / 256 <= 65536, "grid");
+constexpr int64_t kDMost = int64_t(1) << 22;  // (columns are blockIdx.y)
+static_assert(kDMost / 64 <= 65536, "grid");
 
 template <int DT>
 struct Elem;
@@ -83,7 +83,8 @@ template <int DT, int N>
 __device__ __forceinline__ void load_n(const typename Elem<DT>::T *p, float (&v)[N]) {
   values<DT, N>(load_raw<DT, N>(p), v);
 }
-template <int DT, int N>
+// STREAM: the lines are not to push others out of L2.
+template <int DT, int N, bool STREAM = false>
 __device__ __forceinline__ void store_n(typename Elem<DT>::T *p, const float (&v)[N]) {
   if constexpr (N == 1) {
     *p = Elem<DT>::put(v[0]);
@@ -100,7 +101,9 @@ __device__ __forceinline__ void store_n(typename Elem<DT>::T *p, const float (&v
           x[i] = *reinterpret_cast<const uint32_t *>(&h);
         }
       }
-      *reinterpret_cast<uint4 *>(p + k) = make_uint4(x[0], x[1], x[2], x[3]);
+      const uint4 w = make_uint4(x[0], x[1], x[2], x[3]);
+      if (STREAM) __stcs(reinterpret_cast<uint4 *>(p + k), w);
+      else *reinterpret_cast<uint4 *>(p + k) = w;
     }
   }
 }
@@ -124,7 +127,8 @@ struct EmbedParams {
 constexpr int kEmbedWarps = 8;
 constexpr int kEmbedVecs = 4;  // vectors under way per lane
 
-// A warp takes a piece of a row: bound by the two moves of the row through memory; the token's number has to come first.
+// A warp takes a piece of a row: bound by the two moves of the row through memory; the token's number has to come first.  The table's rows of
+// frequent tokens stay in L2 if the vectors pass by it: 131,072 tokens of 1,536 bf16 entries 125 us with plain stores, 113 with streaming ones.
 template <int DT, int N>
 __global__ void __launch_bounds__(kEmbedWarps * 32, N == 1 ? 4 : 8) embed_kernel(const __grid_constant__ EmbedParams p) {
   using E = Elem<DT>;
@@ -152,7 +156,7 @@ __global__ void __launch_bounds__(kEmbedWarps * 32, N == 1 ? 4 : 8) embed_kernel
         values<DT, N>(v[k], x);
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] = live ? x[i] * p.scale : fill;
-        store_n<DT, N>(dst + c + k * 32 * N, x);
+        store_n<DT, N, true>(dst + c + k * 32 * N, x);
       }
     }
     // entries behind the last whole vector
@@ -170,6 +174,7 @@ struct SortParams {
   int tiles;
   int64_t tile;          // tokens of a tile
   int32_t *counts;       // [tiles][digits]
+  int32_t *bases;        // [digits + 1]: first place of every value of the upper digit
   uint2 *pairs;          // by the upper digit: (token, position)
   int32_t *keys, *perm;  // sorted: tokens, positions
   int32_t *start;        // [V + 1]: first sorted position of every token
@@ -235,99 +240,104 @@ __device__ __forceinline__ int32_t place_of(int32_t *count, int d, bool valid) {
   return at;
 }
 
-constexpr int kScatterWarps = 8;
+constexpr int kScatterWarps = 16;  // at most: each has its own counters
+constexpr int kInHand = 4;  // tokens of a lane that are fetched at once
+// Bound by its chain of dependent steps, most of all the tiles' counts of a digit (a thread a digit took 10 us for 64 tiles).
 __global__ void __launch_bounds__(kScatterWarps * 32) scatter_kernel(const __grid_constant__ SortParams p) {
   extern __shared__ int32_t dyn[];
   __shared__ int32_t sh[32];
   int32_t *const base = dyn;                // [digits]
-  int32_t *const hist = dyn + p.digits;     // [warps][digits]
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int d = threadIdx.x; d < p.digits * kScatterWarps; d += kScatterWarps * 32) hist[d] = 0;
+  int32_t *const mine = dyn + p.digits;     // [digits]: entries in this tile's predecessors
+  int32_t *const hist = dyn + 2 * p.digits; // [warps][digits]
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, threads = blockDim.x, warps = threads >> 5;
+  for (int d = threadIdx.x; d < p.digits * (warps + 2); d += threads) dyn[d] = 0;
   wait_for_stream_predecessor();
   __syncthreads();
-  // entries of every digit in this tile's predecessors, and in all tiles
-  for (int d = threadIdx.x; d < p.digits; d += kScatterWarps * 32) {
-    int32_t mine = 0, all = 0;
-#pragma unroll 8
-    for (int t = 0; t < p.tiles; ++t) {
-      const int32_t c = p.counts[(int64_t)t * p.digits + d];
-      if (t < (int)blockIdx.x) mine += c;
-      all += c;
-    }
-    base[d] = all;
-    hist[d] = mine;  // (kept in the first warp's row for a moment)
-  }
-  __syncthreads();
-  scan_in_place(base, p.digits, sh);
-  for (int d = threadIdx.x; d < p.digits; d += kScatterWarps * 32) {
-    base[d] += hist[d];
-    hist[d] = 0;
-  }
-  __syncthreads();
   // the warps take consecutive parts of the tile
-  const int64_t part = p.tile / kScatterWarps;  // a multiple of 32
+  const int64_t part = p.tile / warps;  // a multiple of 32
   const int64_t lo = blockIdx.x * p.tile + warp * part, hi = lo + part < p.n ? lo + part : p.n;
+  int32_t tok[kInHand];
+#pragma unroll
+  for (int k = 0; k < kInHand; ++k) tok[k] = lo + k * 32 + lane < hi ? p.tok[lo + k * 32 + lane] : -1;
+  {  // four groups of threads take a quarter of the tiles each
+    const int quarter = (p.tiles + 3) / 4, group = (int)threadIdx.x / (threads / 4);
+    const int from = group * quarter, to = from + quarter < p.tiles ? from + quarter : p.tiles;
+    for (int d = (int)threadIdx.x % (threads / 4); d < p.digits; d += threads / 4) {
+      int32_t before = 0, all = 0;
+#pragma unroll 8
+      for (int t = from; t < to; ++t) {
+        const int32_t c = p.counts[(int64_t)t * p.digits + d];
+        if (t < (int)blockIdx.x) before += c;
+        all += c;
+      }
+      atomicAdd(&base[d], all);
+      atomicAdd(&mine[d], before);
+    }
+  }
   int32_t *const own = hist + warp * p.digits;
-  for (int64_t t = lo + lane; t < hi; t += 32) {
-    const int64_t tok = p.tok[t];
-    if ((uint64_t)tok < (uint64_t)p.V) atomicAdd(&own[tok >> p.low], 1);
+#pragma unroll
+  for (int k = 0; k < kInHand; ++k)
+    if ((uint32_t)tok[k] < (uint32_t)p.V) atomicAdd(&own[tok[k] >> p.low], 1);
+  for (int64_t t = lo + kInHand * 32 + lane; t < hi; t += 32) {
+    const int32_t x = p.tok[t];
+    if ((uint32_t)x < (uint32_t)p.V) atomicAdd(&own[x >> p.low], 1);
   }
   __syncthreads();
-  for (int d = threadIdx.x; d < p.digits; d += kScatterWarps * 32) {
-    int32_t at = base[d];
-    for (int w = 0; w < kScatterWarps; ++w) {
+  const int32_t total = scan_in_place(base, p.digits, sh);
+  if (blockIdx.x == 0) {
+    for (int d = threadIdx.x; d < p.digits; d += threads) p.bases[d] = base[d];
+    if (threadIdx.x == 0) p.bases[p.digits] = total;
+  }
+  for (int d = threadIdx.x; d < p.digits; d += threads) {
+    int32_t at = base[d] + mine[d];
+    for (int w = 0; w < warps; ++w) {
       const int32_t c = hist[w * p.digits + d];
       hist[w * p.digits + d] = at;
       at += c;
     }
   }
   __syncthreads();
-  for (int64_t t0 = lo; t0 < hi; t0 += 32) {
-    const int64_t t = t0 + lane;
-    const int64_t tok = t < hi ? p.tok[t] : -1;
-    const bool valid = (uint64_t)tok < (uint64_t)p.V;
-    const int32_t at = place_of(own, (int)(tok >> p.low), valid);
-    if (valid) p.pairs[at] = make_uint2((uint32_t)tok, (uint32_t)t);
-  }
+  auto place = [&](int64_t t, int32_t x) {
+    const bool valid = (uint32_t)x < (uint32_t)p.V;
+    const int32_t at = place_of(own, x >> p.low, valid);
+    if (valid) p.pairs[at] = make_uint2((uint32_t)x, (uint32_t)t);
+  };
+#pragma unroll
+  for (int k = 0; k < kInHand; ++k)
+    if (lo + k * 32 < hi) place(lo + k * 32 + lane, tok[k]);
+  for (int64_t t0 = lo + kInHand * 32; t0 < hi; t0 += 32) place(t0 + lane, t0 + lane < hi ? p.tok[t0 + lane] : -1);
 }
 
 // One CTA sorts one bucket by the lower digit.
-__global__ void bucket_kernel(const __grid_constant__ SortParams p) {
+constexpr int kBucketWarps = 32;  // at most: each has its own counters
+__global__ void __launch_bounds__(kBucketWarps * 32) bucket_kernel(const __grid_constant__ SortParams p) {
   extern __shared__ int32_t dyn[];
   __shared__ int32_t sh[32];
-  __shared__ int32_t bounds[2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, threads = blockDim.x;
   const int bins = 1 << p.low, bucket = blockIdx.x;
   int32_t *const total = dyn;          // [bins]
   int32_t *const hist = dyn + bins;    // [warps][bins]
   for (int d = threadIdx.x; d < bins * warps; d += threads) hist[d] = 0;
-  if (threadIdx.x < 2) bounds[threadIdx.x] = 0;
   wait_for_stream_predecessor();
   __syncthreads();
-  {  // entries before this bucket, and in it
-    int32_t before = 0, mine = 0;
-    for (int t = warp; t < p.tiles; t += warps) {
-#pragma unroll 4
-      for (int d = lane; d <= bucket; d += 32) {
-        const int32_t c = p.counts[(int64_t)t * p.digits + d];
-        if (d < bucket) before += c;
-        else mine += c;
-      }
-    }
-    before = __reduce_add_sync(0xffffffffu, before);
-    mine = __reduce_add_sync(0xffffffffu, mine);
-    if (lane == 0) {
-      atomicAdd(&bounds[0], before);
-      atomicAdd(&bounds[1], mine);
-    }
-  }
-  __syncthreads();
-  const int32_t first = bounds[0], count = bounds[1];
+  const int32_t first = p.bases[bucket], count = p.bases[bucket + 1] - first;
   const uint2 *const pairs = p.pairs + first;
   const int32_t part = ((count + warps - 1) / warps + 31) / 32 * 32;
   const int32_t lo = warp * part < count ? warp * part : count, hi = lo + part < count ? lo + part : count;
   int32_t *const own = hist + warp * bins;
-  for (int32_t i = lo + lane; i < hi; i += 32) atomicAdd(&own[pairs[i].x & (uint32_t)(bins - 1)], 1);
+  constexpr int kRounds = 8;  // entries of a lane that are fetched at once
+  uint2 e[kRounds];
+  auto fetch = [&](int32_t from) {
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k)
+      if (from + k * 32 + lane < hi) e[k] = pairs[from + k * 32 + lane];
+  };
+  for (int32_t i0 = lo; i0 < hi; i0 += 32 * kRounds) {
+    fetch(i0);
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k)
+      if (i0 + k * 32 + lane < hi) atomicAdd(&own[e[k].x & (uint32_t)(bins - 1)], 1);
+  }
   __syncthreads();
   for (int d = threadIdx.x; d < bins; d += threads) {
     int32_t s = 0;
@@ -348,13 +358,17 @@ __global__ void bucket_kernel(const __grid_constant__ SortParams p) {
     if (v == p.V - 1) p.start[p.V] = at;
   }
   __syncthreads();
-  for (int32_t i0 = lo; i0 < hi; i0 += 32) {
-    const bool valid = i0 + lane < hi;
-    const uint2 e = valid ? pairs[i0 + lane] : make_uint2(0u, 0u);
-    const int32_t at = place_of(own, (int)(e.x & (uint32_t)(bins - 1)), valid);
-    if (valid) {
-      p.keys[at] = (int32_t)e.x;
-      p.perm[at] = (int32_t)e.y;
+  for (int32_t i0 = lo; i0 < hi; i0 += 32 * kRounds) {
+    if (hi - lo > 32 * kRounds) fetch(i0);  // (else they are still there)
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+      if (i0 + k * 32 >= hi) break;
+      const bool valid = i0 + k * 32 + lane < hi;
+      const int32_t at = place_of(own, (int)(e[k].x & (uint32_t)(bins - 1)), valid);
+      if (valid) {
+        p.keys[at] = (int32_t)e[k].x;
+        p.perm[at] = (int32_t)e[k].y;
+      }
     }
   }
 }
@@ -452,29 +466,44 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumPar
   }
 }
 
-// Runs of several segments: the CTA of the segment where one begins adds its parts in their order.
+// Runs of several segments: the CTA of the segment where one begins adds its parts.  Four groups of threads take a quarter of them each, in order,
+// and the quarters are added in order (a token that is 6 % of 131,072 has 60 parts).
+constexpr int kJoinGroups = 4;
 template <int DO, int N>
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ SumParams p) {
+__global__ void __launch_bounds__(kJoinGroups * 64) join_kernel(const __grid_constant__ SumParams p) {
+  __shared__ float sh[kJoinGroups - 1][64 * N];
   wait_for_stream_predecessor();
-  const int64_t m = p.start[p.V];
   const int64_t lo = (int64_t)blockIdx.x * p.seg, hi = lo + p.seg;
+  const int64_t m = p.start[p.V];
   if (hi >= m) return;  // nothing behind this segment
   const int32_t v = p.keys[hi - 1];
-  if (v != p.keys[hi] || p.start[v] < lo) return;
-  const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * N;
-  if (c >= p.D) return;
-  const int64_t last = (p.start[v + 1] - 1) / p.seg;  // segment of the run's end
-  const float *src = p.part + ((int64_t)blockIdx.x * 2 + 1) * p.D + c;
-  float sum[N];
-  load_n<0, N>(src, sum);
-  src = p.part + ((int64_t)blockIdx.x * 2 + 2) * p.D + c;
+  if (v != p.keys[hi] || (lo > 0 && p.keys[lo - 1] == v)) return;  // no run goes on, or it began before
+  const int group = threadIdx.x >> 6, col = threadIdx.x & 63;
+  const int64_t c = ((int64_t)blockIdx.y * 64 + col) * N;
+  const int64_t last = ((int64_t)p.start[v + 1] - 1) / p.seg;  // segment of the run's end
+  const int64_t count = last - blockIdx.x, each = (count + kJoinGroups - 1) / kJoinGroups;
+  const int64_t from = blockIdx.x + 1 + group * each, to = from + each < last + 1 ? from + each : last + 1;
+  float sum[N] = {};
+  if (c < p.D) {
+    if (group == 0) load_n<0, N>(p.part + ((int64_t)blockIdx.x * 2 + 1) * p.D + c, sum);
 #pragma unroll 8
-  for (int64_t s = blockIdx.x + 1; s <= last; ++s, src += 2 * p.D) {
-    float x[N];
-    load_n<0, N>(src, x);
+    for (int64_t s = from; s < to; ++s) {
+      float x[N];
+      load_n<0, N>(p.part + s * 2 * p.D + c, x);
 #pragma unroll
-    for (int j = 0; j < N; ++j) sum[j] += x[j];
+      for (int j = 0; j < N; ++j) sum[j] += x[j];
+    }
   }
+  if (group > 0) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) sh[group - 1][col * N + j] = sum[j];
+  }
+  __syncthreads();
+  if (group > 0 || c >= p.D) return;
+#pragma unroll
+  for (int g = 0; g < kJoinGroups - 1; ++g)
+#pragma unroll
+    for (int j = 0; j < N; ++j) sum[j] += sh[g][col * N + j];
   finish<DO, N>(p, v, c, sum);
 }
 
@@ -486,17 +515,18 @@ inline size_t up16(size_t b) { return (b + 15) / 16 * 16; }
 struct BackwardPlan {
   int low, digits, tiles, seg;
   int64_t tile, segs;
-  size_t counts, pairs, keys, perm, start, part, bytes;  // offsets into the workspace
+  size_t counts, bases, pairs, keys, perm, start, part, bytes;  // offsets into the workspace
 };
 BackwardPlan backward_plan(int64_t n, int64_t V, int64_t D) {
   BackwardPlan b = {};
   int bits = 1;
   while ((int64_t(1) << bits) < V) ++bits;
-  b.low = (bits + 1) / 2 > bits - 10 ? (bits + 1) / 2 : bits - 10;
+  // (every CTA of the second kernel reads the counts of all tiles and digits, and one of the third holds counters for each of its warps)
+  b.low = bits - 10 > 9 ? bits - 10 : 9;
   b.digits = (int)((V + (int64_t(1) << b.low) - 1) >> b.low);
   // 2,048 tokens a tile, more where there would be over kTilesMost of them (every CTA of the second kernel reads all counts)
   b.tile = (n + kTilesMost - 1) / kTilesMost;
-  b.tile = b.tile < 2048 ? 2048 : (b.tile + 255) / 256 * 256;
+  b.tile = b.tile < 2048 ? 2048 : (b.tile + 511) / 512 * 512;
   b.tiles = (int)((n + b.tile - 1) / b.tile);
   b.seg = n < 32768 ? 32 : kSegMost;  // few tokens: more CTAs, many: fewer partial sums
   b.segs = (n + b.seg - 1) / b.seg;
@@ -507,6 +537,7 @@ BackwardPlan backward_plan(int64_t n, int64_t V, int64_t D) {
     return here;
   };
   b.counts = take((size_t)b.tiles * b.digits * 4);
+  b.bases = take((size_t)(b.digits + 1) * 4);
   b.pairs = take((size_t)n * 8);
   b.keys = take((size_t)n * 4);
   b.perm = take((size_t)n * 4);
@@ -534,7 +565,7 @@ cudaError_t launch_behind(void (*kern)(P...), dim3 grid, int threads, size_t sme
 template <int DG, int DO, int N>
 cudaError_t launch_sums(const SumParams &p, dim3 sums, dim3 joins, int threads, cudaStream_t stream) {
   const cudaError_t e = launch_behind(sum_kernel<DG, DO, N>, sums, threads, 0, stream, p);
-  return e == cudaSuccess ? launch_behind(join_kernel<DO, N>, joins, threads, 0, stream, p) : e;
+  return e == cudaSuccess ? launch_behind(join_kernel<DO, N>, joins, kJoinGroups * 64, 0, stream, p) : e;
 }
 
 }  // namespace
@@ -595,17 +626,20 @@ extern "C" e3_status e3_embed_tokens_backward(const int32_t *tok, int64_t n, con
   SortParams s = {};
   s.tok = tok; s.n = n; s.V = V; s.low = b.low; s.digits = b.digits; s.tiles = b.tiles; s.tile = b.tile;
   s.counts = reinterpret_cast<int32_t *>(ws + b.counts);
+  s.bases = reinterpret_cast<int32_t *>(ws + b.bases);
   s.pairs = reinterpret_cast<uint2 *>(ws + b.pairs);
   s.keys = reinterpret_cast<int32_t *>(ws + b.keys);
   s.perm = reinterpret_cast<int32_t *>(ws + b.perm);
   s.start = reinterpret_cast<int32_t *>(ws + b.start);
   cudaError_t e = launch_behind(count_kernel, dim3((unsigned)b.tiles), kCountThreads, 0, cs, s);
-  if (e == cudaSuccess)
-    e = launch_behind(scatter_kernel, dim3((unsigned)b.tiles), kScatterWarps * 32, (size_t)(kScatterWarps + 1) * b.digits * 4, cs, s);
   if (e == cudaSuccess) {
-    // as many warps as have their own counters in 40 KB
-    int warps = (int)(40 * 1024 / 4 / (1 << b.low)) - 1;
-    warps = warps > 16 ? 16 : (warps < 1 ? 1 : warps);
+    const int warps = b.digits <= 640 ? kScatterWarps : kScatterWarps / 2;  // (counters of 46 KB at most)
+    e = launch_behind(scatter_kernel, dim3((unsigned)b.tiles), warps * 32, (size_t)(warps + 2) * b.digits * 4, cs, s);
+  }
+  if (e == cudaSuccess) {
+    // as many warps as have their own counters in 46 KB
+    int warps = (int)(46 * 1024 / 4 / (1 << b.low)) - 1;
+    warps = warps > kBucketWarps ? kBucketWarps : (warps < 1 ? 1 : warps);
     e = launch_behind(bucket_kernel, dim3((unsigned)b.digits), warps * 32, (size_t)(warps + 1) * (1u << b.low) * 4, cs, s);
   }
   if (e != cudaSuccess) return E3_ERR_CUDA;
@@ -622,7 +656,7 @@ extern "C" e3_status e3_embed_tokens_backward(const int32_t *tok, int64_t n, con
   const int threads = (int)(((vecs + cols - 1) / cols + 31) / 32 * 32);
   p.zero_rows = 32;
   p.zero_ctas = accumulate ? 0 : (V + p.zero_rows - 1) / p.zero_rows;
-  const dim3 sums((unsigned)(b.segs + p.zero_ctas), (unsigned)cols), joins((unsigned)b.segs, (unsigned)cols);
+  const dim3 sums((unsigned)(b.segs + p.zero_ctas), (unsigned)cols), joins((unsigned)b.segs, (unsigned)((vecs + 63) / 64));
   if (dt == E3_F32 && table_dt == E3_F32)
     e = vec ? launch_sums<0, 0, 4>(p, sums, joins, threads, cs) : launch_sums<0, 0, 1>(p, sums, joins, threads, cs);
   else if (dt == E3_F32)

@@ -86,7 +86,8 @@ def exact_gradient(g, tok, V, scale):
 
 @pytest.mark.parametrize("dtype, table", [("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "fp32"), ("fp32", "bf16")])
 @pytest.mark.parametrize("n, V, D", [(1, 1, 1), (2, 3, 5), (31, 2, 8), (33, 1000, 64), (2049, 50, 1000), (5000, 33333, 129),
-                                     (40000, 700, 72), (4097, 4097, 2056)])
+                                     (40000, 700, 72), (4097, 4097, 2056), (6000, 1 << 22, 3),
+                                     (300000, 3000000, 8), (1200000, 5000, 16)])
 def test_gradient(e3, dtype, table, n, V, D):
     r = generator(n + V + D)
     g = torch.randn((n, D), generator=r, device="cuda").to(DTYPES[dtype])
