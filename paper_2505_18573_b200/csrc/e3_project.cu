@@ -70,10 +70,22 @@ __device__ __forceinline__ void mbar_arrive(u64 *b) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(b)) : "memory");
 }
 // Waits for a phase; false after the limit, or once another thread of the CTA has given up.  (The global timer is slow to read: not before some polls.)
+template <bool CLUSTER>
+__device__ __forceinline__ bool poll(u64 *b, uint32_t parity) {
+  if (!CLUSTER) return mbar_try_wait(b, parity);
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_addr(b)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+template <bool CLUSTER = false>
 __device__ __noinline__ bool wait_longer(u64 *b, uint32_t parity, int *gave_up, u64 limit) {
   u64 t0 = 0;
   for (uint32_t it = 0;; ++it) {
-    if (mbar_try_wait(b, parity)) return true;
+    if (poll<CLUSTER>(b, parity)) return true;
     if ((it & 63u) == 63u) {
       const u64 now = global_ns();
       if (t0 == 0) t0 = now;
@@ -84,8 +96,9 @@ __device__ __noinline__ bool wait_longer(u64 *b, uint32_t parity, int *gave_up, 
     }
   }
 }
+template <bool CLUSTER = false>  // CLUSTER: another CTA of the cluster arrives there
 __device__ __forceinline__ bool wait_for(u64 *b, uint32_t parity, int *gave_up, u64 limit) {
-  return mbar_try_wait(b, parity) || wait_longer(b, parity, gave_up, limit);
+  return poll<CLUSTER>(b, parity) || wait_longer<CLUSTER>(b, parity, gave_up, limit);
 }
 // One lane of the warp, always the same.  Loops whose copies and products one lane issues are run by the whole warp: their operands sit in uniform
 // registers, and with a lane's own branch around the loop the compiler has to bring each there by a loop over the lanes (800 cycles a block).
@@ -94,8 +107,9 @@ __device__ __forceinline__ bool elected() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
   return is != 0;
 }
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool wait_as_warp(u64 *b, uint32_t parity, int *gave_up, u64 limit) {
-  return __all_sync(0xffffffffu, wait_for(b, parity, gave_up, limit));
+  return __all_sync(0xffffffffu, wait_for<CLUSTER>(b, parity, gave_up, limit));
 }
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y, u64 *bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
@@ -339,18 +353,31 @@ constexpr int kCols = 128;             // columns of a thread
 constexpr int kAhead = 2;              // blocks whose scales are fetched together
 constexpr int kSumWarps = 4 * kN / kCols;
 constexpr int kThreads = (kSumWarps + 2) * 32;
-constexpr int kStageBytes = (kM + kN) * kTileK;
-constexpr int kStages = 4;
-// Finished logits go through shared memory, 64 bytes of each of a warp's 32 rows at a time, so that they leave in pieces of rows.
-constexpr int kPieceBytes = 64, kPieces = 32 * kPieceBytes;
-constexpr size_t kSmem = (size_t)kStages * kStageBytes + kSumWarps * 2 * kPieces + 1024;
-static_assert(kSmem + 512 <= 227 * 1024, "shared memory");
+// A CTA alone has a tile to itself; a pair of CTAs shares the products of 256 rows x 256 entries, each with its own 128 rows of sums and half of the
+// entries' operand in its shared memory.
+template <bool PAIR>
+struct Ring {
+  static constexpr int kEntries = PAIR ? kN / 2 : kN;  // of the table, in this CTA
+  static constexpr int kStageBytes = (kM + kEntries) * kTileK;
+  static constexpr int kStages = PAIR ? 5 : 3;
+};
+// Finished logits leave through shared memory: 128 bytes of each of a warp's 32 rows at a time, swizzled, which one thread then sends off as a whole while
+// the warp goes on (its own loads and stores of them, beside the products' and copies' use of the same memory, took 3,100 cycles a tile).
+constexpr int kPieceBytes = 128, kPieces = 32 * kPieceBytes;
+constexpr int kOutBytes = 2 * kPieces;  // of a warp
+template <bool PAIR>
+constexpr size_t kSmem = (size_t)Ring<PAIR>::kStages * Ring<PAIR>::kStageBytes + kSumWarps * kOutBytes + 1024;
+static_assert(kSmem<false> + 512 <= 227 * 1024 && kSmem<true> + 512 <= 227 * 1024, "shared memory");
 
-// Where 16 bytes of a row lie: spread so that neither eight rows' first parts nor two rows' four parts meet in a bank.
-__device__ __forceinline__ uint32_t piece_at(int row, int part) { return (uint32_t)(row * kPieceBytes + ((part ^ ((row >> 1) & 3)) << 4)); }
+// Where 16 bytes of a row lie (the 128-byte swizzle).
+__device__ __forceinline__ uint32_t piece_at(int row, int part) { return (uint32_t)(row * kPieceBytes + ((part ^ (row & 7)) << 4)); }
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
+}
 
+template <bool PAIR>
 struct Shared {
-  u64 full[kStages], empty[kStages];
+  u64 full[Ring<PAIR>::kStages], empty[Ring<PAIR>::kStages];  // full, of a pair: in the first CTA, for the copies of both
   u64 sum_full[kBuffers], sum_empty[kBuffers];
   u64 drained;
   uint32_t tmem;
@@ -380,11 +407,51 @@ __device__ __forceinline__ uint32_t bf16_pair(f2 v) {
   return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-template <int OUT>
+// Products of a pair of CTAs: issued by its first one, they read both CTAs' operands and write both CTAs' tensor memory.
+__device__ __forceinline__ void multiply_pair(uint32_t d, u64 a, u64 b, uint32_t form, uint32_t add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+      "l"(b), "r"(form), "r"(add)
+      : "memory");
+}
+// Arrives on `bar` of both CTAs, or of this one, once the pair's products so far are done.
+__device__ __forceinline__ void commit_pair_to_both(u64 *bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)),
+               "h"((unsigned short)3)
+               : "memory");
+}
+__device__ __forceinline__ void commit_pair(u64 *bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+// Shared-memory address of the pair's first CTA.
+__device__ __forceinline__ uint32_t in_first(const void *p) {
+  uint32_t to;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(to) : "r"(smem_addr(p)));
+  return to;
+}
+// Arrives on the barrier of the pair's first CTA, behind the thread's reads of tensor memory.  (With release at cluster scope the arrival waits
+// for the warp's logits under way: 1,500 cycles a block.)
+__device__ __forceinline__ void arrive_at_first(u64 *b) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(in_first(b)) : "memory"); }
+// A copy into this CTA whose bytes count on a barrier of the pair's first CTA.
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+template <int OUT, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
-    project_rows_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ ProjectParams p) {
+    project_rows_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap out_map,
+                        const __grid_constant__ ProjectParams p) {
+  constexpr int kStages = Ring<PAIR>::kStages, kStageBytes = Ring<PAIR>::kStageBytes;
+  constexpr int kRows = PAIR ? 2 * kM : kM;  // of a tile
   extern __shared__ unsigned char dyn[];
-  __shared__ Shared sh;
+  __shared__ Shared<PAIR> sh;
+  const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u, first_tile = PAIR ? blockIdx.x >> 1 : blockIdx.x, tile_step = PAIR ? gridDim.x >> 1 : gridDim.x;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const uint32_t ring = (smem_addr(dyn) + 1023u) & ~1023u;
   if (tid == 0) {
@@ -394,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < kBuffers; ++i) {
       mbar_init(&sh.sum_full[i], 1);
-      mbar_init(&sh.sum_empty[i], kSumWarps);
+      mbar_init(&sh.sum_empty[i], PAIR ? 2 * kSumWarps : kSumWarps);
     }
     mbar_init(&sh.drained, 1);
     sh.gave_up = 0;
@@ -402,11 +469,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_async_smem();
   }
   if (warp == kSumWarps + 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&sh.tmem)), "r"(kBuffers * kN) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    if (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&sh.tmem)), "r"(kBuffers * kN) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&sh.tmem)), "r"(kBuffers * kN) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
     fence_before();
   }
   __syncthreads();
+  if (PAIR) cluster_barrier();  // (the other CTA's barriers stand, and its tensor memory is there)
   fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -417,21 +490,28 @@ __global__ void __launch_bounds__(kThreads, 1)
     {
       uint32_t n = 0;
       bool on = true;
-      for (uint32_t tile = blockIdx.x; tile < p.tiles && on; tile += gridDim.x) {
-        const int tv = (int)(tile / p.row_tiles) * kN, tr = (int)(tile % p.row_tiles) * kM;
+      for (uint32_t tile = first_tile; tile < p.tiles && on; tile += tile_step) {
+        const int tv = (int)(tile / p.row_tiles) * kN + (int)rank * Ring<PAIR>::kEntries, tr = (int)(tile % p.row_tiles) * kRows + (int)rank * kM;
         for (int k = 0; k < p.blocks && on; ++k, ++n) {
           const uint32_t s = n % kStages, round = n / kStages;
           on = wait_as_warp(&sh.empty[s], (round & 1u) ^ 1u, &sh.gave_up, p.wait_ns);
           if (!on) break;
           const uint32_t at = ring + s * kStageBytes;
           if (elected()) {
-            mbar_arrive_expect(&sh.full[s], kStageBytes);
-            tma_load(at, &x_map, k * kTileK, tr, &sh.full[s]);
-            tma_load(at + kM * kTileK, &w_map, k * kTileK, tv, &sh.full[s]);
+            if (PAIR) {
+              if (rank == 0) mbar_arrive_expect(&sh.full[s], 2 * kStageBytes);
+              const uint32_t bar = in_first(&sh.full[s]);
+              tma_load_pair(at, &x_map, k * kTileK, tr, bar);
+              tma_load_pair(at + kM * kTileK, &w_map, k * kTileK, tv, bar);
+            } else {
+              mbar_arrive_expect(&sh.full[s], kStageBytes);
+              tma_load(at, &x_map, k * kTileK, tr, &sh.full[s]);
+              tma_load(at + kM * kTileK, &w_map, k * kTileK, tv, &sh.full[s]);
+            }
           }
         }
       }
-      if (!on && lane == 0) {  // given up: the copies under way still land in this CTA's memory
+      if (!on && lane == 0 && rank == 0) {  // given up: the copies under way still land in this CTA's memory (and the other's)
         for (uint32_t m = n > kStages ? n - kStages : 0; m < n; ++m) {
           const u64 t0 = global_ns();
           while (!mbar_try_wait(&sh.full[m % kStages], (m / kStages) & 1u) && global_ns() - t0 < p.wait_ns) {
@@ -442,41 +522,52 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp == kSumWarps + 1) {
     // ---- issuer of the products
     {
-      constexpr uint32_t kForm = 1u << 4 | (uint32_t)(kN >> 3) << 17 | (uint32_t)(kM >> 4) << 24;
+      constexpr uint32_t kForm = 1u << 4 | (uint32_t)(kN >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
       uint32_t n = 0;
       bool on = true;
-      for (uint32_t tile = blockIdx.x; tile < p.tiles && on; tile += gridDim.x) {
+      if (rank != 0) on = false;  // (a pair's products are issued by its first CTA)
+      for (uint32_t tile = first_tile; tile < p.tiles && on; tile += tile_step) {
         for (int k = 0; k < p.blocks && on; ++k, ++n) {
           const uint32_t s = n % kStages, round = n / kStages, half = n % kBuffers;
           // both waits at once, as a rule there is nothing to wait for
-          const bool here = mbar_try_wait(&sh.sum_empty[half], ((n / kBuffers) & 1u) ^ 1u), there = mbar_try_wait(&sh.full[s], round & 1u);
-          if (!__all_sync(0xffffffffu, here && there))
-            on = wait_as_warp(&sh.sum_empty[half], ((n / kBuffers) & 1u) ^ 1u, &sh.gave_up, p.wait_ns) &&
-                 wait_as_warp(&sh.full[s], round & 1u, &sh.gave_up, p.wait_ns);
+          const uint32_t free_parity = ((n / kBuffers) & 1u) ^ 1u, here_parity = round & 1u;
+          const bool free = poll<PAIR>(&sh.sum_empty[half], free_parity), here = poll<PAIR>(&sh.full[s], here_parity);
+          if (!__all_sync(0xffffffffu, free && here))
+            on = wait_as_warp<PAIR>(&sh.sum_empty[half], free_parity, &sh.gave_up, p.wait_ns) &&
+                 wait_as_warp<PAIR>(&sh.full[s], here_parity, &sh.gave_up, p.wait_ns);
           if (!on) break;
           fence_after();
           const uint32_t at = ring + s * kStageBytes;
           const u64 a = operand(at), b = operand(at + kM * kTileK);
           if (elected()) {
 #pragma unroll
-            for (int i = 0; i < kTileK / 32; ++i) multiply(tmem + half * kN, a + (u64)(2 * i), b + (u64)(2 * i), kForm, i > 0);
-            commit(&sh.sum_full[half]);
+            for (int i = 0; i < kTileK / 32; ++i) {
+              if (PAIR) multiply_pair(tmem + half * kN, a + (u64)(2 * i), b + (u64)(2 * i), kForm, i > 0);
+              else multiply(tmem + half * kN, a + (u64)(2 * i), b + (u64)(2 * i), kForm, i > 0);
+            }
+            if (PAIR) commit_pair_to_both(&sh.sum_full[half]);
+            else commit(&sh.sum_full[half]);
           }
         }
       }
       // products under way (there are some if the CTA has given up) write the tensor memory, and their signals its shared memory
-      if (elected()) commit(&sh.drained);
-      __syncwarp();
-      const u64 t0 = global_ns();
-      while (!mbar_try_wait(&sh.drained, 0) && global_ns() - t0 < p.wait_ns) {
+      if (rank == 0) {
+        if (elected()) {
+          if (PAIR) commit_pair(&sh.drained);
+          else commit(&sh.drained);
+        }
+        __syncwarp();
+        const u64 t0 = global_ns();
+        while (!mbar_try_wait(&sh.drained, 0) && global_ns() - t0 < p.wait_ns) {
+        }
       }
     }
   } else {
     // ---- sums: a thread has one row and kCols vocabulary entries
     constexpr int kEsize = OUT == 0 ? 4 : 2, kPieceCols = kPieceBytes / kEsize;
-    const int group = warp >> 2, row_of_warp = (warp & 3) * 32;
+    const int group = warp >> 2, row_of_warp = (int)rank * kM + (warp & 3) * 32;
     const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + group * kCols;  // (lane 32 (warp mod 4) of the tensor memory)
-    const uint32_t piece = ring + kStages * kStageBytes + warp * 2 * kPieces;
+    const uint32_t piece = ring + kStages * kStageBytes + warp * kOutBytes;
     uint32_t n = 0;
     bool on = true;
     // scales of four blocks ahead, the next tile's first ones too: the row's, and the table's for these entries (multiplied when they are needed, or
@@ -485,7 +576,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const float *sx, *sw, *next_sx, *next_sw;
     auto point_at = [&](uint32_t tile, const float *&sx, const float *&sw) {
       const uint32_t tv = tile / p.row_tiles;
-      const int64_t r = (int64_t)(tile - tv * p.row_tiles) * kM + row_of_warp + lane;
+      const int64_t r = (int64_t)(tile - tv * p.row_tiles) * kRows + row_of_warp + lane;
       sx = p.x_scale + (r < p.rows ? r : 0) * p.x_scale_stride;
       const int64_t block = ((int64_t)tv * kN + group * kCols) / E3_SCALE_BLOCK;  // (a tile may reach past the last)
       sw = p.w_scale + (block * E3_SCALE_BLOCK < p.V ? block : 0) * p.w_scale_stride;
@@ -506,17 +597,17 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     };
     static_assert(E3_SCALE_BLOCK % kCols == 0, "one scale of the table a thread and block");
-    point_at(blockIdx.x, next_sx, next_sw);
+    point_at(first_tile < p.tiles ? first_tile : 0, next_sx, next_sw);
     sx = next_sx;
     sw = next_sw;
     fetch(0);
-    for (uint32_t tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
+    for (uint32_t tile = first_tile; tile < p.tiles; tile += tile_step) {
       const int64_t v0 = (int64_t)(tile / p.row_tiles) * kN + group * kCols;
-      const int64_t r0 = (int64_t)(tile % p.row_tiles) * kM + row_of_warp;
+      const int64_t r0 = (int64_t)(tile % p.row_tiles) * kRows + row_of_warp;
       // the next tile's scales are on their way while this one is summed: from memory they take as long as three blocks
-      const bool more = tile + gridDim.x < p.tiles;
+      const bool more = tile + tile_step < p.tiles;
       if (more) {
-        point_at(tile + gridDim.x, next_sx, next_sw);
+        point_at(tile + tile_step, next_sx, next_sw);
         for (int k = 0; k < p.blocks; k += 32) {
           asm volatile("prefetch.global.L1 [%0];" ::"l"(next_sx + k));
           asm volatile("prefetch.global.L1 [%0];" ::"l"(next_sw + k));
@@ -543,7 +634,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const u64 c2 = (u64)bits << 32 | bits;
         scale[0] = scale[1];
         const uint32_t half = n % kBuffers;
-        on = wait_as_warp(&sh.sum_full[half], (n / kBuffers) & 1u, &sh.gave_up, p.wait_ns);
+        on = wait_as_warp<PAIR>(&sh.sum_full[half], (n / kBuffers) & 1u, &sh.gave_up, p.wait_ns);
         if (!on) break;
         // (the products have read their operands too)
         if (warp == 0 && lane == 0) mbar_arrive(&sh.empty[n % kStages]);
@@ -556,7 +647,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (q + 1 == kCols / 16) {
             fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.sum_empty[half]);
+            if (lane == 0) {
+              if (PAIR) arrive_at_first(&sh.sum_empty[half]);
+              else mbar_arrive(&sh.sum_empty[half]);
+            }
           }
 #pragma unroll
           for (int i = 0; i < 8; ++i) add_scaled(sum[q * 8 + i], t[2 * i], t[2 * i + 1], c2);
@@ -567,67 +661,78 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int i = 0; i < kCols / 2; ++i) sum[i] = 0x7FC000007FC00000ull;
       }
-      const int left = (int)(p.rows - r0 < 32 ? p.rows - r0 : 32);  // rows of this warp
+      const int left = (int)(p.rows - r0 < 32 ? (p.rows > r0 ? p.rows - r0 : 0) : 32);  // rows of this warp
       char *const to = static_cast<char *>(p.out) + (r0 * p.out_stride + v0) * kEsize;
       const int64_t row_bytes = p.out_stride * kEsize;
-      char *const mine = to + (lane >> 2) * row_bytes + (lane & 3) * 16;  // of this lane's 16 bytes of the first eight rows
-      const bool whole = p.vectors != 0 && left == 32 && v0 + kCols <= p.V;
 #pragma unroll
       for (int q = 0; q < kCols / kPieceCols; q += 2) {
+        if (p.vectors) {  // (what was sent before has left)
+          if (elected()) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        }
         __syncwarp();
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < 8; ++i) {
             uint32_t w[4];
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
               if (OUT == 1) {
-                w[h] = bf16_pair(pair_of(sum[(q + j) * 16 + i * 4 + h]));
+                w[h] = bf16_pair(pair_of(sum[(q + j) * 32 + i * 4 + h]));
               } else {
-                const f2 x = pair_of(sum[(q + j) * 8 + i * 2 + (h >> 1)]);
+                const f2 x = pair_of(sum[(q + j) * 16 + i * 2 + (h >> 1)]);
                 w[h] = __float_as_uint((h & 1) != 0 ? x.y : x.x);
               }
             }
             sts128(piece + (uint32_t)(j * kPieces) + piece_at(lane, i), w[0], w[1], w[2], w[3]);
           }
         }
-        __syncwarp();
-        if (whole) {
-          uint4 x[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = lds128(piece + (uint32_t)((i >> 2) * kPieces) + piece_at((i & 3) * 8 + (lane >> 2), lane & 3));
-#pragma unroll
-          for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4 *>(mine + (i & 3) * 8 * row_bytes + (q + (i >> 2)) * kPieceBytes) = x[i];
-        } else {
-          const int col = lane % kPieceCols, step = 32 / kPieceCols;
+        if (p.vectors) {
+          fence_async_smem();
+          __syncwarp();
+          if (elected()) {
+            if (left > 0) {  // (rows and entries behind the last are left out by the copy)
+              if (v0 + q * kPieceCols < p.V) tma_store(&out_map, (int)v0 + q * kPieceCols, (int)r0, piece);
+              if (v0 + (q + 1) * kPieceCols < p.V) tma_store(&out_map, (int)v0 + (q + 1) * kPieceCols, (int)r0, piece + kPieces);
+            }
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          }
+        } else {  // rows that begin anywhere
+          __syncwarp();
 #pragma unroll 1
           for (int j = 0; j < 2; ++j) {
-            if (v0 + (q + j) * kPieceCols + col >= p.V) continue;
-#pragma unroll 4
-            for (int rr = lane / kPieceCols; rr < left; rr += step) {
-              const uint32_t at = piece + (uint32_t)(j * kPieces) + piece_at(rr, col * kEsize >> 4) + (uint32_t)(col * kEsize & 15);
-              char *const there = to + rr * row_bytes + ((q + j) * kPieceCols + col) * kEsize;
-              if (OUT == 0) {
-                *reinterpret_cast<float *>(there) = lds_elem<0>(at);
-              } else {
-                unsigned short h;
-                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at));
-                *reinterpret_cast<unsigned short *>(there) = h;
+#pragma unroll 1
+            for (int col = lane; col < kPieceCols; col += 32) {
+              if (v0 + (q + j) * kPieceCols + col >= p.V) break;
+              char *there = to + ((q + j) * kPieceCols + col) * kEsize;
+#pragma unroll 8
+              for (int rr = 0; rr < left; ++rr, there += row_bytes) {
+                const uint32_t at = piece + (uint32_t)(j * kPieces) + piece_at(rr, col * kEsize >> 4) + (uint32_t)(col * kEsize & 15);
+                if (OUT == 0) {
+                  *reinterpret_cast<float *>(there) = lds_elem<0>(at);
+                } else {
+                  unsigned short h;
+                  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at));
+                  *reinterpret_cast<unsigned short *>(there) = h;
+                }
               }
             }
           }
         }
       }
     }
+    if (p.vectors && elected()) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    __syncwarp();
     if (!on && lane == 0 && p.status != nullptr) atomicOr(p.status, kStatusTimeout);
   }
   fence_before();
   __syncthreads();
+  if (PAIR) cluster_barrier();  // (the other CTA's products and signals reach into this one)
   if (warp == kSumWarps + 1) {
     __syncwarp();
     fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kBuffers * kN));
+    if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kBuffers * kN));
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kBuffers * kN));
   }
 }
 
@@ -656,6 +761,15 @@ bool make_map(Encode encode, CUtensorMap *map, const void *data, int64_t rows, i
   const cuuint32_t boxes[2] = {(cuuint32_t)kTileK, (cuuint32_t)box}, steps[2] = {1, 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(data), size, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The logits, sent 32 rows by 128 bytes at a time.
+bool make_out_map(Encode encode, CUtensorMap *map, void *data, int64_t rows, int64_t cols, int64_t stride, int out) {
+  const int es = out == 0 ? 4 : 2;
+  const cuuint64_t size[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)(stride * es)};
+  const cuuint32_t boxes[2] = {(cuuint32_t)(128 / es), 32}, steps[2] = {1, 1};
+  return encode(map, out == 0 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, data, size, strides, boxes, steps,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // SMs of the current device; 0 where that cannot be told.
@@ -716,43 +830,60 @@ cudaError_t launch(Call &c, cudaStream_t stream) {
   return cudaLaunchKernelEx(&cfg, kern, w_map, x_map, c.p);
 }
 
-template <int OUT>
+template <int OUT, bool PAIR>
 cudaError_t launch_wide(Call &c, cudaStream_t stream) {
+  using R = wide::Ring<PAIR>;
   static std::mutex lock;
-  static bool ready[64];
-  auto kern = wide::project_rows_kernel<OUT>;
+  static int held[64];  // CTAs, or pairs of them, that the device holds
+  auto kern = wide::project_rows_kernel<OUT, PAIR>;
   int dev = 0;
   const int sms = sm_count(dev);
   if (sms == 0) return cudaErrorInvalidDevice;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(wide::kThreads);
+  cfg.dynamicSmemBytes = wide::kSmem<PAIR>;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = PAIR ? 2 : 1;
   {
     std::lock_guard<std::mutex> hold(lock);
-    if (!ready[dev]) {
-      const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)wide::kSmem);
+    if (held[dev] == 0) {
+      cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)wide::kSmem<PAIR>);
       if (e != cudaSuccess) return e;
-      ready[dev] = true;
+      int n = sms;
+      if (PAIR) {
+        cudaLaunchConfig_t one = cfg;
+        one.gridDim = dim3(2);
+        one.attrs = attr + 1;
+        one.numAttrs = 1;
+        one.stream = nullptr;
+        e = cudaOccupancyMaxActiveClusters(&n, kern, &one);
+        if (e != cudaSuccess) return e;
+        if (n < 1) return cudaErrorInvalidConfiguration;
+      }
+      held[dev] = n;
     }
   }
   const Encode encode = encode_function();
-  CUtensorMap w_map, x_map;
-  if (encode == nullptr || !make_map(encode, &w_map, c.w, c.p.V, c.D, c.w_stride, wide::kN) ||
-      !make_map(encode, &x_map, c.x, c.p.rows, c.D, c.x_stride, wide::kM))
+  CUtensorMap w_map, x_map, out_map = {};
+  if (encode == nullptr || !make_map(encode, &w_map, c.w, c.p.V, c.D, c.w_stride, R::kEntries) ||
+      !make_map(encode, &x_map, c.x, c.p.rows, c.D, c.x_stride, wide::kM) ||
+      (c.p.vectors && !make_out_map(encode, &out_map, c.p.out, c.p.rows, c.p.V, c.p.out_stride, OUT)))
     return cudaErrorInvalidValue;
-  c.p.row_tiles = (c.p.rows + wide::kM - 1) / wide::kM;
+  const int rows = PAIR ? 2 * wide::kM : wide::kM;
+  c.p.row_tiles = (uint32_t)((c.p.rows + rows - 1) / rows);
   const int64_t tiles = (int64_t)((c.p.V + wide::kN - 1) / wide::kN) * c.p.row_tiles;
   if (tiles >= (int64_t)1 << 31) return cudaErrorInvalidValue;
   c.p.tiles = (uint32_t)tiles;
   c.p.wait_ns = kDefaultWaitNs;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(tiles < sms ? tiles : sms));
-  cfg.blockDim = dim3(wide::kThreads);
-  cfg.dynamicSmemBytes = wide::kSmem;
-  cfg.stream = stream;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kern, x_map, w_map, c.p);
+  cfg.gridDim = dim3((unsigned)(tiles < held[dev] ? tiles : held[dev]) * (PAIR ? 2u : 1u));
+  return cudaLaunchKernelEx(&cfg, kern, x_map, w_map, out_map, c.p);
 }
 
 template <int OUT>
@@ -760,7 +891,8 @@ cudaError_t launch_sized(Call &c, cudaStream_t stream) {
   if (c.p.rows <= 16) return launch<16, OUT>(c, stream);
   if (c.p.rows <= 32) return launch<32, OUT>(c, stream);
   if (c.p.rows <= 64) return launch<64, OUT>(c, stream);
-  return launch_wide<OUT>(c, stream);
+  if (c.p.rows <= wide::kM) return launch_wide<OUT, false>(c, stream);
+  return launch_wide<OUT, true>(c, stream);
 }
 
 }  // namespace
