@@ -85,7 +85,7 @@ def exact_gradient(g, tok, V, scale):
 
 
 @pytest.mark.parametrize("dtype, table", [("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "fp32"), ("fp32", "bf16")])
-@pytest.mark.parametrize("n, V, D", [(1, 1, 1), (2, 3, 5), (31, 2, 8), (33, 1000, 64), (2049, 50, 1000), (5000, 33333, 129),
+@pytest.mark.parametrize("n, V, D", [(1, 1, 1), (2, 3, 5), (31, 2, 8), (33, 1000, 64), (2049, 50, 1000), (4096, 70, 19), (4097, 70, 19), (129, 31, 2), (4000, 33, 1), (5000, 33333, 129),
                                      (40000, 700, 72), (4097, 4097, 2056), (6000, 1 << 22, 3),
                                      (300000, 3000000, 8), (1200000, 5000, 16)])
 def test_gradient(e3, dtype, table, n, V, D):
@@ -109,7 +109,7 @@ def test_gradient(e3, dtype, table, n, V, D):
 
 def test_gradient_of_one_hot_token(e3):
     """All tokens alike: one run over every segment."""
-    for n in (31, 32, 33, 64, 5000, 40000):
+    for n in (31, 32, 33, 64, 128, 129, 4096, 4097, 5000, 40000):
         g = torch.randn((n, 40), generator=generator(n), device="cuda")
         got = e3.e3_embed_tokens_backward(g, torch.full((n,), 3, device="cuda", dtype=torch.int32), 5)
         want, size, count = exact_gradient(g, torch.full((n,), 3, device="cuda"), 5, 1.0)
@@ -117,7 +117,7 @@ def test_gradient_of_one_hot_token(e3):
 
 
 def test_gradient_of_padding_alone_and_of_no_tokens(e3):
-    for n in (0, 1, 700):
+    for n in (0, 1, 700, 6000):
         tok = torch.full((n,), -1, device="cuda", dtype=torch.int32)
         tok[::2] = 99  # outside the vocabulary
         got = e3.e3_embed_tokens_backward(torch.ones((n, 12), device="cuda"), tok, 9, out=torch.full((9, 12), 5.0, device="cuda"))
