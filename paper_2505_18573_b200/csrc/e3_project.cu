@@ -511,7 +511,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       }
-      if (!on && lane == 0 && rank == 0) {  // given up: the copies under way still land in this CTA's memory (and the other's)
+      if (!on && lane == 0 && rank != 0) {  // given up: this CTA's copies count in the other; they land well within a millisecond
+        const u64 t0 = global_ns();
+        while (global_ns() - t0 < 1000000u) {
+        }
+      }
+      if (!on && lane == 0 && rank == 0) {  // the copies under way still land in this CTA's memory (and the other's)
         for (uint32_t m = n > kStages ? n - kStages : 0; m < n; ++m) {
           const u64 t0 = global_ns();
           while (!mbar_try_wait(&sh.full[m % kStages], (m / kStages) & 1u) && global_ns() - t0 < p.wait_ns) {

@@ -977,7 +977,7 @@ __global__ void __launch_bounds__(kThreads, 4) draw_kernel(const __grid_constant
     return finish(tok);
   }
   int kind = w.kind;
-  float floor = lead.lo;  // a score that some block reaches
+  float floor = kind == kNoDraft ? reached_p - 1e-5f : lead.lo;  // a score that some block reaches (ln Z is in it)
   for (int round = 0; round < 2; ++round) {
     Exact e = {0.0, INT_MAX};
     for (int i0 = warp * 32; i0 < p.blocks; i0 += kThreads) {

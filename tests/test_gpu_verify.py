@@ -267,7 +267,7 @@ def test_uniforms_next_to_the_ratio(e3, sign):
 def test_blocks_and_entries_next_to_each_other(e3, sign):
     """Two leading blocks, and a prefix sum and the uniform, closer than sums in fp32 can tell."""
     for model in (True, False):
-        s = Batch(10, 12, 1, 3000, model=model)
+        s = Batch(10, 12, 1, 2800, model=model)
         s.uniforms[:, 0] = 1 - 1e-12  # refused nearly everywhere
         tok, kept, _, _ = reference(s)
         z, u = host(s.logits), host(s.uniforms)
@@ -281,8 +281,8 @@ def test_blocks_and_entries_next_to_each_other(e3, sign):
                     p = np.maximum(p - np.exp((y - y[d]) / float(s.draft_temps[b]) + float(s.draft_logp[b, 0])), 0)
                 else:
                     p[d] = 0
-            full = np.zeros(3072)
-            full[:3000] = p
+            full = np.zeros(11 * BLOCK)
+            full[:2800] = p
             sums = full.reshape(-1, BLOCK).sum(1)
             score = np.log(sums) - np.log(-np.log(u[b, 1:-1]))
             first, second = np.argsort(-score)[:2]
@@ -293,6 +293,23 @@ def test_blocks_and_entries_next_to_each_other(e3, sign):
                 prefix = np.cumsum(part) / part.sum()
                 s.uniforms[b, -1] = min(max(prefix[100] * (1 + sign * 1e-9), 0.0), 1 - 1e-9)
         s.check(e3)
+
+
+def test_a_rare_block_next_to_a_confident_one(e3):
+    """A row whose best token has all but 5e-5 of the mass, and a block of those 5e-5 whose uniform brings it next to the best token's."""
+    deltas = [d * s for d in (1e-7, 1e-6, 3e-6, 1e-5) for s in (1, -1)]
+    for far in (-9.5, -9.9, -10.4):
+        s = Batch(21, len(deltas), 0, 64 * BLOCK)
+        s.draft_logits = s.draft_temps = s.draft_logp = None
+        s.logits.fill_(-300.0)
+        s.logits[:, 5], s.logits[:, 32 * BLOCK + 7] = 0.0, far
+        s.temps.fill_(1.0)
+        s.uniforms.fill_(0.5)
+        s.uniforms[:, 0] = math.exp(-1.0)  # (a variate of zero)
+        for b, delta in enumerate(deltas):
+            s.uniforms[b, 32] = math.exp(-math.exp(float(np.float32(far)) + delta))
+        tok = s.check(e3)[0].cpu().numpy()[:, 0]
+        assert [int(t) for t in tok] == [5 if d > 0 else 32 * BLOCK + 7 for d in deltas]
 
 
 def test_outputs_given_and_left_out(e3):
