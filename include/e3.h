@@ -260,7 +260,7 @@ E3_API e3_status e3_embed_tokens(const int32_t *tok, int64_t n, const void *tabl
  *   g           device, type dt, [n, D] with g_stride elements from row to row
  *   dtable      device, type table_dt (it may be wider than dt), [V, D] with dtable_stride elements from row to row; must not overlap g
  *   workspace   e3_embed_workspace_bytes(n, V, D) bytes of device scratch (0 for sizes that the call rejects, and for n == 0)
- * n < 2^31, V <= 2^22, D < 2^22.
+ * n < 2^31, V <= 2^22, D <= 64 x 65535.
  */
 E3_API size_t e3_embed_workspace_bytes(int64_t n, int64_t V, int64_t D);
 E3_API e3_status e3_embed_tokens_backward(const int32_t *tok, int64_t n, const void *g, e3_dtype dt, int64_t V, int64_t D,

@@ -19,8 +19,7 @@ constexpr int kDigitsMost = 1024;    // buckets of the upper digit
 constexpr int kLowMost = 12;         // bits of the lower digit
 constexpr int kTilesMost = 512;
 constexpr int64_t kVMost = int64_t(kDigitsMost) << kLowMost;
-constexpr int64_t kDMost = int64_t(1) << 22;  // (columns are blockIdx.y)
-static_assert(kDMost / 64 <= 65536, "grid");
+constexpr int64_t kDMost = int64_t(65535) * 64;  // (64 columns a CTA, as blockIdx.y)
 
 template <int DT>
 struct Elem;
@@ -373,26 +372,36 @@ __global__ void __launch_bounds__(kBucketWarps * 32) bucket_kernel(const __grid_
   }
 }
 
-constexpr int kZeroRows = 32;  // rows of the table that a CTA looks at
-// Zeroes the rows v0 + b for the bits b of `which`, a warp each, in 16-byte vectors whatever they begin on.
-__device__ __forceinline__ void zero_rows(char *out, int64_t v0, uint32_t which, int64_t D, int64_t stride, int esize) {
+constexpr int kZeroRows = 32;  // rows of the table that are looked at together
+// Zeroes the rows v0 + b for the bits b of `which`, in 16-byte vectors whatever they begin on, L lanes a row.
+template <int L>
+__device__ __forceinline__ void zero_rows_by(char *out, int64_t v0, uint32_t which, int64_t D, int64_t stride, int esize) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  for (int b = warp; b < kZeroRows; b += warps) {
+  const int64_t bytes = D * esize;
+  const int l = lane % L;
+  for (int b = warp * (32 / L) + lane / L; b < kZeroRows; b += warps * (32 / L)) {
     if ((which >> b & 1u) == 0u) continue;
     char *const row = out + (v0 + b) * stride * esize;
-    const int64_t bytes = D * esize;
     int64_t head = (16 - (int64_t)(reinterpret_cast<uintptr_t>(row) & 15u)) & 15;
     if (head > bytes) head = bytes;
     const int64_t vecs = (bytes - head) / 16, tail = head + vecs * 16;
     uint4 *const mid = reinterpret_cast<uint4 *>(row + head);
-    for (int64_t i = lane; i < vecs; i += 32) __stcs(mid + i, make_uint4(0u, 0u, 0u, 0u));
-    // fewer than eight entries before and behind
-    const int64_t at = lane < 8 ? lane * esize : tail + (lane - 8) * esize;
-    if (lane < 8 ? at < head : (lane < 16 && at < bytes)) {
+    for (int64_t i = l; i < vecs; i += L) __stcs(mid + i, make_uint4(0u, 0u, 0u, 0u));
+#pragma unroll
+    for (int i = l; i < 16; i += L) {  // fewer than eight entries before and behind
+      const int64_t at = i < 8 ? i * esize : tail + (i - 8) * esize;
+      if (i < 8 ? at >= head : at >= bytes) continue;
       if (esize == 4) *reinterpret_cast<uint32_t *>(row + at) = 0u;
       else *reinterpret_cast<uint16_t *>(row + at) = 0;
     }
   }
+}
+
+// (A warp a row of 64 bytes took three times as long for a table of 2^22 of them.)
+__device__ __forceinline__ void zero_rows(char *out, int64_t v0, uint32_t which, int64_t D, int64_t stride, int esize) {
+  if (D * esize > 512) zero_rows_by<32>(out, v0, which, D, stride, esize);
+  else if (D * esize > 64) zero_rows_by<8>(out, v0, which, D, stride, esize);
+  else zero_rows_by<4>(out, v0, which, D, stride, esize);
 }
 
 // ---- few tokens ---------------------------------------------------------------------------------------------------
@@ -401,6 +410,9 @@ __device__ __forceinline__ void zero_rows(char *out, int64_t v0, uint32_t which,
 // (3,001 tokens of 1001 fp32 into 33,333 rows: 35 us for the whole gradient, 50 with the three kernels above, whose steps wait for one
 // another; zeroing in the summing kernel's launch instead took 44, its row loads queueing behind the stores.)
 constexpr int kFew = 4096;
+// A CTA that zeroes looks through the tokens for groups of 32 rows: one, or as many (32 at most) as make up kZeroBytes, or short rows of a large table
+// cost more looks than bytes (4,096 tokens, 2^22 rows of 16 fp32: 805 us with one).
+constexpr int kZeroGroupsMost = 32, kZeroBytes = 32 * 1024;
 constexpr int kRankThreads = 512, kRankEach = 16, kRankTokens = kRankThreads / kRankEach;  // threads that compare for a token, tokens of a CTA
 struct FewParams {
   const int32_t *tok;
@@ -410,27 +422,29 @@ struct FewParams {
   // CTAs behind the first rank_ctas zero the rows of tokens that do not occur
   char *out;
   int64_t D, out_stride;
-  int esize, rank_ctas;
+  int esize, rank_ctas, zero_groups;
 };
 __global__ void __launch_bounds__(kRankThreads) few_kernel(const __grid_constant__ FewParams p) {
   __shared__ __align__(16) int32_t key[kFew];
   const int tid = threadIdx.x;
   wait_for_stream_predecessor();
   if ((int)blockIdx.x >= p.rank_ctas) {
-    const int64_t v0 = (int64_t)((int)blockIdx.x - p.rank_ctas) * kZeroRows;
-    if (tid == 0) key[0] = 0;
+    const int rows = p.zero_groups * kZeroRows;
+    const int64_t v0 = (int64_t)((int)blockIdx.x - p.rank_ctas) * rows;
+    if (tid < p.zero_groups) key[tid] = 0;  // a bit a row
     __syncthreads();
-    uint32_t seen = 0u;
 #pragma unroll 4
     for (int t = tid; t < p.n; t += kRankThreads) {
       const int64_t at = (int64_t)p.tok[t] - v0;
-      if ((uint64_t)at < kZeroRows) seen |= 1u << at;
+      if ((uint64_t)at < (uint64_t)rows) atomicOr(&key[at >> 5], (int32_t)(1u << (at & 31)));
     }
-    seen = __reduce_or_sync(0xffffffffu, seen);
-    if ((tid & 31) == 0 && seen != 0u) atomicOr(&key[0], (int32_t)seen);
     __syncthreads();
-    const uint32_t there = p.V - v0 < kZeroRows ? (1u << (p.V - v0)) - 1u : 0xffffffffu;
-    zero_rows(p.out, v0, ~(uint32_t)key[0] & there, p.D, p.out_stride, p.esize);
+    for (int g = 0; g < p.zero_groups; ++g) {
+      const int64_t v = v0 + g * kZeroRows;
+      if (v >= p.V) break;
+      const uint32_t there = p.V - v < kZeroRows ? (1u << (p.V - v)) - 1u : 0xffffffffu;
+      zero_rows(p.out, v, ~(uint32_t)key[g] & there, p.D, p.out_stride, p.esize);
+    }
     return;
   }
   constexpr int32_t kNone = 0x7fffffff;  // tokens outside the vocabulary come last
@@ -483,7 +497,6 @@ struct SumParams {
   float *part;     // [segments][2][D]: of the run that came from the segment before, of the one that goes on behind it
   int64_t segs;
   int seg;         // sorted positions of a segment
-  int64_t zero_ctas;
 };
 
 constexpr int kSegMost = 128;
@@ -698,7 +711,7 @@ extern "C" e3_status e3_embed_tokens(const int32_t *tok, int64_t n, const void *
 }
 
 extern "C" size_t e3_embed_workspace_bytes(int64_t n, int64_t V, int64_t D) {
-  if (n <= 0 || n >= (int64_t(1) << 31) || V < 1 || V > kVMost || D < 1 || D >= kDMost) return 0;
+  if (n <= 0 || n >= (int64_t(1) << 31) || V < 1 || V > kVMost || D < 1 || D > kDMost) return 0;
   return backward_plan(n, V, D).bytes;
 }
 
@@ -707,7 +720,7 @@ extern "C" e3_status e3_embed_tokens_backward(const int32_t *tok, int64_t n, con
                                               int64_t dtable_stride, int accumulate, void *workspace, size_t workspace_bytes,
                                               void *stream) {
   if ((dt != E3_F32 && dt != E3_BF16) || (table_dt != E3_F32 && table_dt != E3_BF16)) return E3_ERR_DTYPE;
-  if (n < 0 || n >= (int64_t(1) << 31) || V < 1 || V > kVMost || D < 1 || D >= kDMost || dtable_stride < D || (n > 0 && g_stride < D))
+  if (n < 0 || n >= (int64_t(1) << 31) || V < 1 || V > kVMost || D < 1 || D > kDMost || dtable_stride < D || (n > 0 && g_stride < D))
     return E3_ERR_INVALID_ARG;
   if (n == 0 && accumulate) return E3_OK;
   if (!dtable || (n > 0 && (!tok || !g))) return E3_ERR_INVALID_ARG;
@@ -725,12 +738,15 @@ extern "C" e3_status e3_embed_tokens_backward(const int32_t *tok, int64_t n, con
   int32_t *const keys = reinterpret_cast<int32_t *>(ws + b.keys), *const perm = reinterpret_cast<int32_t *>(ws + b.perm);
   int32_t *const live = reinterpret_cast<int32_t *>(ws + b.bases), *const start = reinterpret_cast<int32_t *>(ws + b.start);
   const bool few = n <= kFew;
-  const int64_t zero_ctas = accumulate ? 0 : (V + kZeroRows - 1) / kZeroRows;
   cudaError_t e = cudaSuccess;
   if (few) {
     FewParams f = {};
     f.tok = tok; f.n = (int)n; f.V = V; f.keys = keys; f.perm = perm; f.live = live;
     f.out = static_cast<char *>(dtable); f.D = D; f.out_stride = dtable_stride; f.esize = table_dt == E3_BF16 ? 2 : 4;
+    const int64_t group = kZeroRows * D * f.esize, groups = kZeroBytes / group;
+    f.zero_groups = (int)(groups < 1 ? 1 : (groups > kZeroGroupsMost ? kZeroGroupsMost : groups));
+    const int rows = f.zero_groups * kZeroRows;
+    const int64_t zero_ctas = accumulate ? 0 : (V + rows - 1) / rows;
     f.rank_ctas = (int)((n + kRankTokens - 1) / kRankTokens);
     e = launch_behind(few_kernel, dim3((unsigned)(f.rank_ctas + zero_ctas)), kRankThreads, 0, cs, f);
   } else {
@@ -764,8 +780,7 @@ extern "C" e3_status e3_embed_tokens_backward(const int32_t *tok, int64_t n, con
   const int64_t vecs = vec ? D / n_vec : D;
   const int64_t cols = (vecs + 255) / 256;
   const int threads = (int)(((vecs + cols - 1) / cols + 31) / 32 * 32);
-  p.zero_ctas = few ? 0 : zero_ctas;
-  const dim3 sums((unsigned)(b.segs + p.zero_ctas), (unsigned)cols), joins((unsigned)b.segs, (unsigned)((vecs + 63) / 64));
+  const dim3 sums((unsigned)(b.segs + (few || accumulate ? 0 : (V + kZeroRows - 1) / kZeroRows)), (unsigned)cols), joins((unsigned)b.segs, (unsigned)((vecs + 63) / 64));
   if (dt == E3_F32 && table_dt == E3_F32)
     e = vec ? launch_sums<0, 0, 4>(p, sums, joins, threads, cs) : launch_sums<0, 0, 1>(p, sums, joins, threads, cs);
   else if (dt == E3_F32)

@@ -86,6 +86,7 @@ def exact_gradient(g, tok, V, scale):
 
 @pytest.mark.parametrize("dtype, table", [("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "fp32"), ("fp32", "bf16")])
 @pytest.mark.parametrize("n, V, D", [(1, 1, 1), (2, 3, 5), (31, 2, 8), (33, 1000, 64), (2049, 50, 1000), (4096, 70, 19), (4097, 70, 19), (129, 31, 2), (4000, 33, 1), (5000, 33333, 129),
+                                     (4000, 70000, 4), (4097, 70000, 4), (300, 5001, 130), (5000, 5001, 130), (900, 1 << 22, 5), (1000, 2000, 300),
                                      (40000, 700, 72), (4097, 4097, 2056), (6000, 1 << 22, 3),
                                      (300000, 3000000, 8), (1200000, 5000, 16)])
 def test_gradient(e3, dtype, table, n, V, D):

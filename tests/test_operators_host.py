@@ -53,7 +53,8 @@ def test_embed_refuses(e3, change, status):
 
 @pytest.mark.parametrize("change, status", [
     (dict(dt=7), "DTYPE"), (dict(table_dt=7), "DTYPE"), (dict(n=-1), "INVALID_ARG"), (dict(n=1 << 31), "INVALID_ARG"), (dict(V=0), "INVALID_ARG"),
-    (dict(V=(1 << 22) + 1), "INVALID_ARG"), (dict(D=0), "INVALID_ARG"), (dict(D=1 << 22, g_stride=1 << 22, dtable_stride=1 << 22), "INVALID_ARG"),
+    (dict(V=(1 << 22) + 1), "INVALID_ARG"), (dict(D=0), "INVALID_ARG"), (dict(D=64 * 65535 + 1, g_stride=1 << 22, dtable_stride=1 << 22), "INVALID_ARG"),
+    (dict(D=1 << 22, g_stride=1 << 22, dtable_stride=1 << 22), "INVALID_ARG"),
     (dict(g_stride=15), "INVALID_ARG"), (dict(dtable_stride=15), "INVALID_ARG"), (dict(tok=None), "INVALID_ARG"), (dict(g=None), "INVALID_ARG"),
     (dict(dtable=None), "INVALID_ARG"), (dict(g=P + 1), "ALIGNMENT"), (dict(dtable=P + 2), "ALIGNMENT"), (dict(workspace=P + 4), "ALIGNMENT"),
     (dict(workspace=None), "WORKSPACE"), (dict(workspace_bytes=16), "WORKSPACE"), (dict(n=0, accumulate=1, dtable=None), None)])
