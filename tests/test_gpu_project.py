@@ -56,6 +56,39 @@ def test_against_products_in_64_bits(e3, dtype, rows, V, D):
     check(e3, operands(rows + V + D, rows, V, D), dtype)
 
 
+def test_one_entry_at_a_time_with_scales(e3):
+    """Every scale in its place: one entry of each operand's row and block, the scales powers of two that differ from their neighbours'."""
+    rows, V, D = 300, 520, 1100
+    x, w = torch.zeros((rows, 1104), device="cuda"), torch.zeros((V, 1104), device="cuda")
+    for blk in range(9):
+        x[torch.arange(rows, device="cuda"), torch.minimum(torch.tensor(1099, device="cuda"), 128 * blk + torch.arange(rows, device="cuda") % 128)] = 1.0
+        w[:, min(128 * blk + 5, 1099)] = 1.0
+    x, w = x.to(E4M3)[:, :D], w.to(E4M3)[:, :D]
+    sx = torch.exp2((torch.arange(rows, device="cuda")[:, None] * 3 + torch.arange(9, device="cuda")[None] * 5).remainder(11).float() - 5)
+    sw = torch.exp2((torch.arange(5, device="cuda")[:, None] * 2 + torch.arange(9, device="cuda")[None] * 7).remainder(13).float() - 6)
+    for dtype in (torch.float32, torch.bfloat16):
+        got = e3.e3_project_vocab(x, sx, w, sw, dtype=dtype)
+        assert torch.equal(got, (values(x, sx, 1) @ values(w, sw, 128).t()).to(dtype))
+
+
+def test_scales_of_any_value(e3):
+    """Zeros, negative and subnormal scales multiply like others; NaN reaches the rows and entries of its block and no others."""
+    for rows in (40, 100, 200):
+        for at, value in ((0, 0.0), (7, -2.0), (3, 1e-40), (5, 3.0)):
+            for which in (1, 3):
+                ops = operands(9, rows, 600, 500)
+                ops[which].view(-1)[at] = value
+                check(e3, ops, torch.float32)
+        ops = operands(9, rows, 600, 500)
+        ops[1][17, 2] = float("nan")
+        ops[3][1, 0] = float("nan")
+        got = e3.e3_project_vocab(*ops, dtype=torch.float32)
+        nan = torch.zeros((rows, 600), dtype=torch.bool, device="cuda")
+        nan[17] = True
+        nan[:, 128:256] = True
+        assert torch.equal(got.isnan(), nan)
+
+
 def test_many_tiles_a_block(e3):
     """More tiles than SMs, so that the rings run on from tile to tile."""
     for rows in (1, 20, 40, 100, 300):
