@@ -46,11 +46,11 @@ struct VerifyPart {
   int pad[3];
 };
 struct VerifyRow {
-  double lnZ;
-  float R, ent, logp;  // logp: of the draft
-  int state, best, pad;
+  double lnZ, lnq;
+  float R, ent, logp, y;  // logp: of the draft; y, lnq, kind, tok: the draft's, for the draw
+  int state, best, kind, tok;
 };
-static_assert(sizeof(VerifyPart) == 32 && sizeof(VerifyRow) == 32, "records");
+static_assert(sizeof(VerifyPart) == 32 && sizeof(VerifyRow) == 48, "records");
 
 struct VerifyParams {
   const char *logits, *draft_logits;
@@ -73,6 +73,11 @@ struct VerifyParams {
 __device__ __forceinline__ void wait_for_stream_predecessor() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+// The draw's CTAs start once all of the rows' have come this far: what lies before the call is done then.
+__device__ __forceinline__ void wait_for_stream_predecessor_first() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 __device__ __forceinline__ int length_of(const VerifyParams &p, int64_t b) {
   const int64_t n = p.draft_len != nullptr ? (int64_t)p.draft_len[b] : p.drafts;
@@ -372,7 +377,7 @@ __device__ __noinline__ void decide(const VerifyParams &p, int64_t r, int64_t b,
   if (greedy) best_of_warp(s.R, best);
   else join_lanes<32>(s, c);
   if (lane != 0) return;
-  VerifyRow w = {0.0, s.R, 0.f, 0.f, kRefused, best, 0};
+  VerifyRow w = {0.0, d.lnq, s.R, 0.f, 0.f, d.y, kRefused, best, d.kind, d.tok};
   if (bad || !(s.R > -CUDART_INF_F) || (!greedy && !(s.Z > 0.f)) || !usable_uniform(u)) {
     w.state = kInvalid;
   } else if (greedy) {
@@ -408,7 +413,7 @@ __global__ void __launch_bounds__(kRowThreads, kHeld) verify_rows_kernel(const _
   __shared__ int sh_best[kRowWarps], sh_bad[kRowWarps];
   const int lane = threadIdx.x & 31, warp = __shfl_sync(kAll, threadIdx.x >> 5, 0);
   const Place at = place_of(p, blockIdx.x);
-  wait_for_stream_predecessor();
+  wait_for_stream_predecessor_first();
   const int len = length_of(p, at.b);
   const float tau = p.temps[at.b];
   // (no position before it is refused; all warps see the same)
@@ -630,8 +635,9 @@ __device__ __forceinline__ void merge(Lead &l, const Lead &o) {
 }
 __device__ __forceinline__ Lead no_lead() { return Lead{-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, INT_MAX, INT_MAX, 0}; }
 
-// Gumbel variate -ln(-ln u) of a uniform, good to a few units of fp32.
+// Gumbel variate -ln(-ln u) of a uniform, good to a few units of fp32; NaN for one that cannot be used.
 __device__ __forceinline__ float gumbel_of(double u) {
+  if (!usable_uniform(u)) return CUDART_NAN_F;
   const float w = u < 0.5 ? (u > 1e-30 ? -logf((float)u) : (float)-log(u)) : -log1pf((float)(u - 1.0));
   return -logf(w);
 }
@@ -741,9 +747,8 @@ __device__ __noinline__ bool draw_in(const DrawRow &w, int kind, int b, double u
 struct Score {
   float y, off;  // value, bound on its error
 };
-__device__ __forceinline__ Score score_of_p(const float2 &s, double v, float R, float tau, int &bad) {
-  if (!usable_uniform(v)) bad = 1;
-  const float x = s.x > 0.f ? __fdiv_rn(fmaxf(s.y - R, -kFarBelow), tau) : -CUDART_INF_F, y = logf(s.x) + x + gumbel_of(v);
+__device__ __forceinline__ Score score_of_p(const float2 &s, float gumbel, float R, float tau) {
+  const float x = s.x > 0.f ? __fdiv_rn(fmaxf(s.y - R, -kFarBelow), tau) : -CUDART_INF_F, y = logf(s.x) + x + gumbel;
   return Score{y, 1.2e-5f + 2e-6f * (fabsf(x) < 1e3f ? fabsf(x) : 1e3f)};
 }
 
@@ -817,7 +822,7 @@ __device__ __forceinline__ Lead lead_of_warp(Lead l) {
 }
 
 struct DrawShared {
-  float score[kScoresKept];  // of the first blocks, under p: upper bounds
+  float gumbel[kScoresKept], score[kScoresKept];  // of the first blocks: variates, and upper bounds of the scores under p
   Lead lead[kWarps], all;
   Exact exact[kWarps];
   double sum[2 * kWarps];
@@ -836,17 +841,29 @@ __device__ __forceinline__ Lead lead_of_cta(const Lead &l, DrawShared &sh) {
   return sh.all;
 }
 
-// A CTA draws for a sequence: a chain of dependent loads and small reductions, so all that depends on the position alone is fetched at once.
-template <int DT>
-__global__ void __launch_bounds__(kThreads, 4) draw_kernel(const __grid_constant__ VerifyParams p) {
+// A CTA draws for a sequence: a chain of dependent loads, small reductions and code that is met once, so what hangs on the call's inputs alone (the
+// variates of all blocks) is done beside the last rows, and what the decision knew of the draft comes with its record.
+// CTAS of an SM: 4, or the 2 that calls of few sequences need, with as many registers as the draw asks for (64 sequences of 4 drafts, 151,936 bf16: 43 us
+// for the whole call, 45.5 with 4; 512 sequences of 3: 118 us with 2, 114 with 4).
+template <int DT, int CTAS>
+__global__ void __launch_bounds__(kThreads, CTAS) draw_kernel(const __grid_constant__ VerifyParams p) {
   __shared__ DrawShared sh;
   const int tid = threadIdx.x, warp = __shfl_sync(kAll, tid >> 5, 0), lane = tid & 31;
   const int64_t b = blockIdx.x;
   if (tid == 0) sh.reached = enc_neg_inf();
-  wait_for_stream_predecessor();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // What the call was given may be read beside the last rows (the rows' CTAs have all begun behind it): the blocks' variates are ready when the sums are.
+  const double *const u = p.uniforms + b * p.u_stride + p.drafts;
+  const float tau = __ldcg(p.temps + b), tau_d = p.draft_temps != nullptr ? __ldcg(p.draft_temps + b) : tau;
+  const double u_in = __ldcg(u + p.blocks);
+  const int kept = p.blocks < kScoresKept ? p.blocks : kScoresKept;
+  if (tau != 0.f) {
+#pragma unroll 1
+    for (int i = tid; i < kept; i += kThreads) sh.gumbel[i] = gumbel_of(__ldcg(u + i));
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int len = length_of(p, b);
   const int first = p.first[b];
-  const float tau = p.temps[b];
   int a = first < len ? first : len;
   const int64_t r0 = b * (p.drafts + 1);
   auto exact_total = [&](const char *row, float R) { return block_sum(exact_terms<DT>(row, p.V, R, tau, tid, kThreads), sh.sum); };
@@ -859,9 +876,8 @@ __global__ void __launch_bounds__(kThreads, 4) draw_kernel(const __grid_constant
       if (q.state != kNear) continue;
       const char *const row = p.logits + (r0 + j) * p.row_bytes;
       const double lnZ = log(exact_total(row, q.R));
-      const Draft d = draft_of<DT>(p, b, j);
-      const double lp = ((double)load_elem<DT>(row, d.tok) - (double)q.R) * (1.0 / (double)tau) - lnZ;
-      if (p.uniforms[b * p.u_stride + j] * exp(d.lnq) < exp(lp)) continue;
+      const double lp = ((double)load_elem<DT>(row, q.tok) - (double)q.R) * (1.0 / (double)tau) - lnZ;
+      if (p.uniforms[b * p.u_stride + j] * exp(q.lnq) < exp(lp)) continue;
       a = j;
       rec = q;
       rec.lnZ = lnZ;
@@ -887,40 +903,25 @@ __global__ void __launch_bounds__(kThreads, 4) draw_kernel(const __grid_constant
   if (tau == 0.f) return write(rec.best, 0.f, 0.f);
   DrawRow w = {};
   w.z = p.logits + r * p.row_bytes;
-  w.V = p.V; w.tau = tau; w.R = rec.R; w.lnZ = rec.lnZ; w.kind = kNoDraft; w.d = -1;
-  const double *const u = p.uniforms + b * p.u_stride + p.drafts;
-  const float2 *const sums = p.sums + r * p.blocks;
-  const double u_in = u[p.blocks];
-  // ---- scores under p: of the draw itself, or upper bounds (the first ones under way while the draft is looked up)
-  constexpr int kAhead = 4;
-  float2 sum[kAhead];
-  double v[kAhead];
-#pragma unroll
-  for (int k = 0; k < kAhead; ++k) {
-    const int i = tid + k * kThreads;
-    if (i < p.blocks) {
-      sum[k] = __ldcg(sums + i);
-      v[k] = u[i];
-    }
-  }
-  if (a < len) {
-    const Draft d = draft_of<DT>(p, b, a);
-    w.kind = d.kind; w.d = d.tok; w.y_d = d.y; w.lnq = d.lnq;
-    if (d.kind == kDistribution) {
-      w.beta_d = 1.0 / (double)d.tau; w.cd = __fdiv_rn(kLog2e, d.tau); w.nq = (float)(d.lnq * (1.0 / kLn2));
-    }
+  w.V = p.V; w.tau = tau; w.R = rec.R; w.lnZ = rec.lnZ; w.kind = rec.kind; w.d = rec.tok; w.y_d = rec.y; w.lnq = rec.lnq;
+  if (w.kind == kDistribution) {
     w.y = p.draft_logits + (b * p.drafts + a) * p.draft_row_bytes;
+    w.beta_d = 1.0 / (double)tau_d; w.cd = __fdiv_rn(kLog2e, tau_d); w.nq = (float)(rec.lnq * (1.0 / kLn2));
   }
+  const float2 *const sums = p.sums + r * p.blocks;
+  // ---- scores under p: of the draw itself, or upper bounds (a loop of one copy: a CTA runs through most of this once, and waits for its instructions)
   Lead lead = no_lead();
-  auto enter = [&](int i, const float2 &s, double x) {
-    const Score y = score_of_p(s, x, w.R, w.tau, lead.bad);
+  auto score_at = [&](int i, const float2 &s) { return score_of_p(s, i < kScoresKept ? sh.gumbel[i] : gumbel_of(u[i]), w.R, w.tau); };
+  float2 sum = tid < p.blocks ? __ldcg(sums + tid) : make_float2(0.f, 0.f);
+#pragma unroll 1
+  for (int i = tid; i < p.blocks; i += kThreads) {
+    const float2 s = sum;
+    if (i + kThreads < p.blocks) sum = __ldcg(sums + i + kThreads);
+    const Score y = score_at(i, s);
+    lead.bad |= y.y != y.y;
     if (i < kScoresKept) sh.score[i] = y.y + y.off;
     insert(lead, y.y - y.off, y.y + y.off, i);
-  };
-#pragma unroll
-  for (int k = 0; k < kAhead; ++k)
-    if (tid + k * kThreads < p.blocks) enter(tid + k * kThreads, sum[k], v[k]);
-  for (int i = tid + kAhead * kThreads; i < p.blocks; i += kThreads) enter(i, __ldcg(sums + i), u[i]);
+  }
   w.beta = 1.0 / (double)tau; w.c = __fdiv_rn(kLog2e, tau); w.nz = -(float)(rec.lnZ * (1.0 / kLn2));
   auto finish = [&](int tok) {
     if (tok < 0) return write(-1, CUDART_NAN_F, CUDART_NAN_F);
@@ -932,10 +933,9 @@ __global__ void __launch_bounds__(kThreads, 4) draw_kernel(const __grid_constant
   const float reached_p = lead.lo - lnz;
   if (w.kind != kNoDraft) {
     // weights p - q: those blocks whose scores of p reach the best known score of p - q
-    int dummy = 0;
     auto bound = [&](int i) {
       if (i < kScoresKept) return sh.score[i];
-      const Score y = score_of_p(__ldcg(sums + i), u[i], w.R, w.tau, dummy);
+      const Score y = score_at(i, __ldcg(sums + i));
       return y.y + y.off;
     };
     Lead mine = no_lead();
@@ -956,7 +956,7 @@ __global__ void __launch_bounds__(kThreads, 4) draw_kernel(const __grid_constant
       // (the two kinds of scores differ by ln Z)
       if (i == INT_MAX || top - lnz + 4e-6f < dec_float(*(volatile int *)&sh.reached)) break;
       float lo, hi;
-      score_block<DT>(w, i, gumbel_of(u[i]), lo, hi);
+      score_block<DT>(w, i, i < kScoresKept ? sh.gumbel[i] : gumbel_of(u[i]), lo, hi);
       insert(mine, lo, hi, i);
       if (lane == 0) atomicMax(&sh.reached, enc_float(lo));
       __syncwarp();
@@ -981,9 +981,8 @@ __global__ void __launch_bounds__(kThreads, 4) draw_kernel(const __grid_constant
   for (int round = 0; round < 2; ++round) {
     Exact e = {0.0, INT_MAX};
     for (int i0 = warp * 32; i0 < p.blocks; i0 += kThreads) {
-      int dummy = 0;
       Score most = {-CUDART_INF_F, 0.f};
-      if (i0 + lane < p.blocks) most = score_of_p(__ldcg(sums + i0 + lane), u[i0 + lane], w.R, w.tau, dummy);
+      if (i0 + lane < p.blocks) most = score_at(i0 + lane, __ldcg(sums + i0 + lane));
       const float hi = most.y + most.off - lnz + 1e-5f;
       uint32_t open = __ballot_sync(kAll, hi > -CUDART_INF_F && hi >= floor);
       while (open != 0u) {
@@ -1066,7 +1065,7 @@ cudaError_t launch_verify(VerifyParams &p, cudaStream_t stream) {
   if (e == cudaSuccess)
     e = launch_behind(verify_rows_kernel<DT>, (unsigned)(rows * p.n_parts), kRowThreads,
                       (size_t)(kRowWarps * warp_bytes<DT>((round + kRowWarps - 1) / kRowWarps)), stream, p);
-  if (e == cudaSuccess) e = launch_behind(draw_kernel<DT>, (unsigned)p.n_seq, kThreads, 0, stream, p);
+  if (e == cudaSuccess) e = launch_behind(p.n_seq <= 2 * 148 ? draw_kernel<DT, 2> : draw_kernel<DT, 4>, (unsigned)p.n_seq, kThreads, 0, stream, p);
   return e;
 }
 
