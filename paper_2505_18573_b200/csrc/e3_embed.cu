@@ -119,48 +119,83 @@ struct EmbedParams {
   void *out;
   int64_t n, V, D, table_stride, out_stride;
   float scale;
-  int64_t segs;  // a row is cut into this many pieces of `len` vectors (a warp each)
-  int len;
+  int segs, len;  // a row is cut into this many pieces of `len` vectors (a warp each, all under way at once)
 };
 
 constexpr int kEmbedWarps = 8;
-constexpr int kEmbedVecs = 4;  // vectors under way per lane
+constexpr int kEmbedVecs = 8;  // vectors of a lane
 
-// A warp takes a piece of a row: bound by the two moves of the row through memory; the token's number has to come first.  The table's rows of
-// frequent tokens stay in L2 if the vectors pass by it: 131,072 tokens of 1,536 bf16 entries 125 us with plain stores, 113 with streaming ones.
+// scale times the entries of a vector, rounded once.
+template <int DT>
+__device__ __forceinline__ uint4 scaled(const uint4 &v, float2 scale) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  if (DT == 0) {
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+      const float2 x = __fmul2_rn(make_float2(__uint_as_float(w[i]), __uint_as_float(w[i + 1])), scale);
+      w[i] = __float_as_uint(x.x);
+      w[i + 1] = __float_as_uint(x.y);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 x = __fmul2_rn(make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u)), scale);
+      const __nv_bfloat162 h = __floats2bfloat162_rn(x.x, x.y);
+      w[i] = *reinterpret_cast<const uint32_t *>(&h);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// A warp takes a piece of a row, eight vectors a lane: bound by the two moves of the row through memory, the token's number has to come first.
+// 131,072 tokens of 1,536 bf16 entries, a third of them frequent ones: 85 us; with four vectors a lane (a row in two pieces) 101, with 32 registers, which
+// eight CTAs an SM leave and which spill, 114.  The rows of frequent tokens stay in L2 if the vectors pass by it (plain stores: 88).  Tokens at random, none
+// twice: the copy rate.
 template <int DT, int N>
-__global__ void __launch_bounds__(kEmbedWarps * 32, N == 1 ? 4 : 8) embed_kernel(const __grid_constant__ EmbedParams p) {
+__global__ void __launch_bounds__(kEmbedWarps * 32, 4) embed_kernel(const __grid_constant__ EmbedParams p) {
   using E = Elem<DT>;
+  using T = typename E::T;
   wait_for_stream_predecessor();
   const int lane = threadIdx.x & 31;
-  const int64_t items = p.n * p.segs;
-  for (int64_t item = (int64_t)blockIdx.x * kEmbedWarps + (threadIdx.x >> 5); item < items; item += (int64_t)gridDim.x * kEmbedWarps) {
-    const int64_t t = item / p.segs, seg = item - t * p.segs;
-    const int64_t tok = p.tok[t];
-    const bool live = (uint64_t)tok < (uint64_t)p.V;
-    const float fill = tok == -1 ? 0.f : CUDART_NAN_F;
-    const int64_t c0 = seg * p.len * N, whole = p.D / N * N;
-    const int64_t c1 = c0 + (int64_t)p.len * N < whole ? c0 + (int64_t)p.len * N : whole;
-    const typename E::T *src = static_cast<const typename E::T *>(p.table) + (live ? tok : 0) * p.table_stride;
-    typename E::T *dst = static_cast<typename E::T *>(p.out) + t * p.out_stride;
-    for (int64_t c = c0 + lane * N; c < c1; c += 32 * N * kEmbedVecs) {
-      Raw<DT, N> v[kEmbedVecs];
+  for (int seg = blockIdx.y; seg < p.segs; seg += gridDim.y) {
+    const int64_t first = (int64_t)seg * p.len, vecs = p.D / N - first;  // of this piece and those behind it
+    const int left = (int)(vecs < p.len ? vecs : p.len) - lane;
+    for (int64_t t = (int64_t)blockIdx.x * kEmbedWarps + (threadIdx.x >> 5); t < p.n; t += (int64_t)gridDim.x * kEmbedWarps) {
+      const int64_t tok = p.tok[t];
+      const bool live = (uint64_t)tok < (uint64_t)p.V;
+      const T *const row = static_cast<const T *>(p.table) + (live ? tok : 0) * p.table_stride, *const src = row + (first + lane) * N;
+      T *const out = static_cast<T *>(p.out) + t * p.out_stride, *const dst = out + (first + lane) * N;
+      const float fill = tok == -1 ? 0.f : CUDART_NAN_F;
+      if constexpr (N == 1) {
+        T v[kEmbedVecs];
 #pragma unroll
-      for (int k = 0; k < kEmbedVecs; ++k)
-        if (live && c + k * 32 * N < c1) v[k] = load_raw<DT, N>(src + c + k * 32 * N);
+        for (int k = 0; k < kEmbedVecs; ++k)
+          if (live && k * 32 < left) v[k] = src[k * 32];
 #pragma unroll
-      for (int k = 0; k < kEmbedVecs; ++k) {
-        if (c + k * 32 * N >= c1) break;
-        float x[N];
-        values<DT, N>(v[k], x);
+        for (int k = 0; k < kEmbedVecs; ++k)
+          if (k * 32 < left) dst[k * 32] = E::put(live ? E::get(v[k]) * p.scale : fill);
+      } else {
+        uint4 v[kEmbedVecs];
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = live ? x[i] * p.scale : fill;
-        store_n<DT, N, true>(dst + c + k * 32 * N, x);
+        for (int k = 0; k < kEmbedVecs; ++k)
+          if (live && k * 32 < left) v[k] = reinterpret_cast<const uint4 *>(src)[k * 32];
+        if (live) {
+          const float2 scale = make_float2(p.scale, p.scale);
+#pragma unroll
+          for (int k = 0; k < kEmbedVecs; ++k)
+            if (k * 32 < left) __stcs(reinterpret_cast<uint4 *>(dst) + k * 32, scaled<DT>(v[k], scale));
+        } else {
+          float x[N];
+#pragma unroll
+          for (int i = 0; i < N; ++i) x[i] = fill;
+#pragma unroll 1
+          for (int k = 0; k * 32 < left; ++k) store_n<DT, N, true>(dst + k * 32 * N, x);
+        }
+        // entries behind the last whole vector
+        const int64_t e = p.D / N * N + lane;
+        if (seg == p.segs - 1 && e < p.D) out[e] = E::put(live ? E::get(row[e]) * p.scale : fill);
       }
     }
-    // entries behind the last whole vector
-    if (N > 1 && seg == p.segs - 1 && whole + lane < p.D)
-      dst[whole + lane] = E::put(live ? E::get(src[whole + lane]) * p.scale : fill);
   }
 }
 
@@ -701,10 +736,10 @@ extern "C" e3_status e3_embed_tokens(const int32_t *tok, int64_t n, const void *
   const bool vec = !misaligned(table, 16) && !misaligned(out, 16) && table_stride * es % 16 == 0 && out_stride * es % 16 == 0 &&
                    D * (int64_t)es >= 16;
   const int64_t vecs = vec ? D / (int64_t)(16 / es) : D;
-  p.segs = (vecs + 32 * kEmbedVecs - 1) / (32 * kEmbedVecs);
+  p.segs = (int)((vecs + 32 * kEmbedVecs - 1) / (32 * kEmbedVecs));
   p.len = (int)(((vecs + p.segs - 1) / p.segs + 31) / 32 * 32);
-  const int64_t ctas = (n * p.segs + kEmbedWarps - 1) / kEmbedWarps, most = 0x7fffffff;
-  const dim3 grid((unsigned)(ctas < most ? ctas : most));
+  const int64_t ctas = (n + kEmbedWarps - 1) / kEmbedWarps, most = 0x7fffffff;
+  const dim3 grid((unsigned)(ctas < most ? ctas : most), (unsigned)(p.segs < 65535 ? p.segs : 65535));
   const cudaError_t e = launch_behind(dt == E3_F32 ? (vec ? embed_kernel<0, 4> : embed_kernel<0, 1>) : (vec ? embed_kernel<1, 8> : embed_kernel<1, 1>),
                                       grid, kEmbedWarps * 32, 0, static_cast<cudaStream_t>(stream), p);
   return e == cudaSuccess ? E3_OK : E3_ERR_CUDA;
