@@ -10,6 +10,8 @@
  * plus the masked mean entropy that drives the temperature scheduler (Sec. 4.2),
  * the group-relative advantage (Eq. "adv") over ragged rollout groups, and two
  * tiny host functions: Algorithm 1 (rollout budget) and Eq. "tp_adj" with annealing.
+ * At both ends of the vocabulary: token embedding and its gradient, 8-bit values, the projection of
+ * hidden states to logits, and the verification of drafted tokens.
  *
  * Conventions for every device call
  *   - "device" pointers are CUDA device pointers owned by the caller; the
