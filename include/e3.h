@@ -494,6 +494,13 @@ E3_API double e3_anneal_target(const e3_sched *s);
 E3_API void e3_test_arm_stall(int64_t tile, uint64_t wait_ns);
 
 /*
+ * The same for the next e3_project_vocab: the copies of block number `block` (of 128 columns, counted over the tiles that the first thread block
+ * takes one after the other) are never issued, and waits give up after wait_ns.  That thread block's (or pair's) unfinished logits read
+ * NaN, the others' are as ever.  One shot; 2^32 - 1 disarms it.
+ */
+E3_API void e3_test_arm_project_stall(uint32_t block, uint64_t wait_ns);
+
+/*
  * For tests: which kernel a row call of this size takes on a device of `sms` SMs that holds clusters of up to `largest_cluster`
  * blocks.  0: the streaming kernel; else the kernel of short calls, with that many blocks per row.  sampler: an e3_sampler, or -1 for
  * e3_token_logp_entropy; masked: whether that call has a mask.  No device call is made.

@@ -32,7 +32,7 @@ EXPORTS = ("e3_status_string", "e3_workspace_bytes", "e3_sample", "e3_token_logp
            "e3_anneal_target", "e3_entropy_gap", "e3_update_temperature_gap", "e3_difficulty_accumulate", "e3_difficulty_rank", "e3_budget_curriculum",
            "e3_test_arm_stall", "e3_test_row_blocks", "e3_probe_read", "e3_sequence_mean_entropy",
            "e3_verify_drafts", "e3_embed_tokens", "e3_embed_workspace_bytes", "e3_embed_tokens_backward", "e3_quantize",
-           "e3_project_vocab")
+           "e3_project_vocab", "e3_test_arm_project_stall")
 
 
 class E3Error(RuntimeError):
@@ -143,6 +143,8 @@ def lib() -> C.CDLL:
         L.e3_test_row_blocks.argtypes = [C.c_int, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
         L.e3_test_arm_stall.restype = None
         L.e3_test_arm_stall.argtypes = [C.c_int64, C.c_uint64]
+        L.e3_test_arm_project_stall.restype = None
+        L.e3_test_arm_project_stall.argtypes = [C.c_uint32, C.c_uint64]
         _lib, _nat = L, _native
     return _lib
 
@@ -373,6 +375,11 @@ def e3_test_arm_stall(tile: int, wait_ns: int) -> None:
     """Test hook: the next row call leaves one 4 KiB tile uncopied (below -1: row ``-2 - tile`` of a short call waits for a part that never comes) and bounds
     its waits by ``wait_ns``; -1 disarms it."""
     lib().e3_test_arm_stall(int(tile), int(wait_ns))
+
+
+def e3_test_arm_project_stall(block: int, wait_ns: int) -> None:
+    """Test hook: the first thread block of the next projection leaves one block of its operands uncopied, and waits give up after ``wait_ns``."""
+    lib().e3_test_arm_project_stall(int(block), int(wait_ns))
 
 
 E3_PROBE_SCRATCH_BYTES = 65536

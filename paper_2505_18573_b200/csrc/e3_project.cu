@@ -42,7 +42,11 @@ struct ProjectParams {
   int vectors;          // the logits' rows begin on 16-byte boundaries
   uint32_t tiles;       // row tiles run fastest: neighbours share the table's rows in L2
   u64 wait_ns;
+  uint32_t stall;       // test hook: the first CTA's copies of this block (counted over its tiles) are never issued
 };
+constexpr uint32_t kNoStall = 0xffffffffu;
+std::atomic<uint32_t> g_stall{kNoStall};
+std::atomic<unsigned long long> g_stall_wait_ns{0};
 
 // NT: rows of the hidden states in a tile (N of the products).
 template <int NT>
@@ -195,6 +199,7 @@ __global__ void __launch_bounds__(Plan<NT>::kThreads, 1)
   if (warp == L::kSumWarps) {
     // ---- producer
     {
+      const uint32_t stall = blockIdx.x == 0 ? p.stall : kNoStall;
       uint32_t n = 0;
       bool on = true;
       for (uint32_t tile = blockIdx.x; tile < p.tiles && on; tile += gridDim.x) {
@@ -204,7 +209,7 @@ __global__ void __launch_bounds__(Plan<NT>::kThreads, 1)
           on = wait_as_warp(&sh.empty[s], (round & 1u) ^ 1u, &sh.gave_up, p.wait_ns);
           if (!on) break;
           const uint32_t at = ring + s * L::kStageBytes;
-          if (elected()) {
+          if (elected() && n != stall) {
             mbar_arrive_expect(&sh.full[s], L::kStageBytes);
             tma_load(at, &w_map, k * kTileK, tv, &sh.full[s]);
             tma_load(at + kTileV * kTileK, &x_map, k * kTileK, tr, &sh.full[s]);
@@ -489,6 +494,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == kSumWarps) {
     // ---- producer
     {
+      const uint32_t stall = blockIdx.x == 0 ? p.stall : kNoStall;
       uint32_t n = 0;
       bool on = true;
       for (uint32_t tile = first_tile; tile < p.tiles && on; tile += tile_step) {
@@ -498,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           on = wait_as_warp(&sh.empty[s], (round & 1u) ^ 1u, &sh.gave_up, p.wait_ns);
           if (!on) break;
           const uint32_t at = ring + s * kStageBytes;
-          if (elected()) {
+          if (elected() && n != stall) {
             if (PAIR) {
               if (rank == 0) mbar_arrive_expect(&sh.full[s], 2 * kStageBytes);
               const uint32_t bar = in_first(&sh.full[s]);
@@ -822,7 +828,6 @@ cudaError_t launch(Call &c, cudaStream_t stream) {
   const int64_t tiles = (int64_t)((c.p.V + kTileV - 1) / kTileV) * c.p.row_tiles;
   if (tiles >= (int64_t)1 << 31) return cudaErrorInvalidValue;
   c.p.tiles = (uint32_t)tiles;
-  c.p.wait_ns = kDefaultWaitNs;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -887,7 +892,6 @@ cudaError_t launch_wide(Call &c, cudaStream_t stream) {
   const int64_t tiles = (int64_t)((c.p.V + wide::kN - 1) / wide::kN) * c.p.row_tiles;
   if (tiles >= (int64_t)1 << 31) return cudaErrorInvalidValue;
   c.p.tiles = (uint32_t)tiles;
-  c.p.wait_ns = kDefaultWaitNs;
   cfg.gridDim = dim3((unsigned)(tiles < held[dev] ? tiles : held[dev]) * (PAIR ? 2u : 1u));
   return cudaLaunchKernelEx(&cfg, kern, x_map, w_map, out_map, c.p);
 }
@@ -924,8 +928,15 @@ extern "C" e3_status e3_project_vocab(const uint8_t *x, const float *x_scale, in
   c.p.x_scale = x_scale; c.p.w_scale = w_scale; c.p.x_scale_stride = x_scale_stride; c.p.w_scale_stride = w_scale_stride;
   c.p.out = logits; c.p.out_stride = row_stride; c.p.status = out_status;
   c.p.rows = (int)rows; c.p.V = (int)V; c.p.blocks = (int)blocks;
+  c.p.stall = g_stall.exchange(kNoStall);
+  c.p.wait_ns = c.p.stall == kNoStall ? kDefaultWaitNs : g_stall_wait_ns.load();
   c.p.vectors = !misaligned(logits, 16) && row_stride * (dt == E3_F32 ? 4 : 2) % 16 == 0;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
   const cudaError_t e = dt == E3_F32 ? launch_sized<0>(c, cs) : launch_sized<1>(c, cs);
   return e == cudaSuccess ? E3_OK : E3_ERR_CUDA;
+}
+
+extern "C" void e3_test_arm_project_stall(uint32_t block, uint64_t wait_ns) {
+  e3::g_stall_wait_ns.store(wait_ns);
+  e3::g_stall.store(block);
 }

@@ -161,6 +161,32 @@ def test_graphs_and_streams(e3):
         assert all(torch.equal(x, y) for x, y in zip(outs + there, want + want))
 
 
+@pytest.mark.parametrize("rows, pairs", [(9, False), (100, False), (300, True)])
+@pytest.mark.parametrize("block", [0, 6, 13])
+def test_a_wait_that_runs_out(e3, rows, pairs, block):
+    """A block whose copies never come: the call returns, the first thread block's unfinished logits read NaN, the status word tells."""
+    ops = operands(12, rows, 150000, 512)  # more tiles than SMs or pairs of them, four blocks each
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    want = e3.e3_project_vocab(*ops, status=status)
+    assert status.item() == 0
+    e3.e3_test_arm_project_stall(block, 5_000_000)  # 5 ms instead of two seconds
+    got = e3.e3_project_vocab(*ops, status=status)
+    torch.cuda.synchronize()
+    assert status.item() & e3.E3_STATUS_TIMEOUT
+    bad = got.isnan()
+    assert torch.equal(got[~bad], want[~bad])
+    # the tile of the stalled block and the later ones of its thread block, no more than all of its tiles
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    width, high, takers = (256, 256, sms // 2) if pairs else (256, 128, sms) if rows > 64 else (128, 16, sms)
+    tiles = -(-150000 // width) * -(-rows // high)
+    most = -(-tiles // (takers * 3 // 4))  # (a device may hold fewer pairs than half its SMs)
+    assert 0 < int(bad.sum()) <= most * width * min(rows, high)
+    if block == 0:
+        assert bool(bad[0, 0])
+    status.zero_()
+    assert torch.equal(e3.e3_project_vocab(*ops, status=status), want) and status.item() == 0
+
+
 def test_refusals(e3):
     x, sx, w, sw = operands(11, 4, 300, 200)
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
