@@ -203,21 +203,6 @@ __device__ __forceinline__ void best_of_warp(float &R, int &best) {
   R = m;
 }
 
-// sum over the row of exp((z - R) / tau) in fp64, of the entries from `from` on in steps of `step`, by one thread.
-template <int DT>
-__device__ __noinline__ double exact_terms(const char *row, int V, float R, float tau, int from, int step) {
-  constexpr int kAhead = 8;
-  const double beta = 1.0 / (double)tau;
-  double s = 0.0;
-  for (int64_t i0 = from; i0 < V; i0 += (int64_t)step * kAhead) {
-    float z[kAhead];
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) z[k] = i0 + (int64_t)k * step < V ? load_elem<DT>(row, i0 + (int64_t)k * step) : -CUDART_INF_F;
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) s += exp(((double)z[k] - (double)R) * beta);
-  }
-  return s;
-}
 __device__ __forceinline__ double block_sum(double v, double *sh /* [warps] */) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
@@ -689,6 +674,62 @@ __device__ __forceinline__ float entry(const Eight<DT> &e, int k) {
   return __uint_as_float((k & 1) != 0 ? w[k >> 1] & 0xFFFF0000u : w[k >> 1] << 16);
 }
 
+// exp((z - R) / tau) in fp64 of all bf16 values of 2^-9 <= |z| < 2^8: a row in bf16 has no others but a few near zero.
+constexpr int kExpLow = (127 - 9) << 7, kExps = 17 << 7;  // pattern of 2^-9, patterns up to 2^8
+// sum over the row of exp((z - R) / tau) in fp64, a thread's part of it, by the whole CTA.  Bound by one SM's fp64 units, and by the latency of what is not
+// under way beside other things: vectors, four sums, no branches but for the few logits that the table does not hold.
+template <int DT>
+__device__ __noinline__ double exact_terms(const char *row, int V, float R, float tau, double *table /* [2 kExps + 1], bf16 */) {
+  constexpr int kAhead = DT == 1 ? 4 : 1;
+  const double beta = 1.0 / (double)tau;
+  if (DT == 1) {
+    __syncthreads();
+#pragma unroll 1
+    for (int i = threadIdx.x; i < 2 * kExps; i += kThreads) {
+      const uint32_t bits = i < kExps ? (uint32_t)(kExpLow + i) : (uint32_t)(kExpLow + i - kExps) | 0x8000u;
+      table[i] = exp(((double)__uint_as_float(bits << 16) - (double)R) * beta);
+    }
+    if (threadIdx.x == 0) table[2 * kExps] = 0.0;
+    __syncthreads();
+  }
+  double s[4] = {};
+#pragma unroll 1
+  for (int64_t i0 = (int64_t)threadIdx.x * 8; i0 < V; i0 += (int64_t)kThreads * 8 * kAhead) {
+    Eight<DT> e[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (i0 + (int64_t)k * kThreads * 8 < V) e[k] = load_eight<DT>(row, V, (int)(i0 + (int64_t)k * kThreads * 8));
+    bool others = false;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int64_t i = i0 + (int64_t)k * kThreads * 8;
+      const int there = i < V ? (V - i < 8 ? (int)(V - i) : 8) : 0;
+      if (DT == 1) {
+#pragma unroll
+        for (int h = 0; h < 8; ++h) {
+          const uint32_t bits = __float_as_uint(entry<DT>(e[k], h)) >> 16, at = (bits & 0x7FFFu) - kExpLow;
+          const bool known = at < (uint32_t)kExps && h < there;
+          others |= !known && h < there;
+          s[h & 3] += table[known ? at + ((bits & 0x8000u) != 0u ? kExps : 0) : 2 * kExps];
+        }
+      } else {
+#pragma unroll
+        for (int h = 0; h < 8; ++h) s[h & 3] += h < there ? exp(((double)entry<DT>(e[k], h) - (double)R) * beta) : 0.0;
+      }
+    }
+    if (DT == 1 && others) {
+#pragma unroll 1
+      for (int n = 0; n < 8 * kAhead; ++n) {
+        const int64_t i = i0 + (int64_t)(n >> 3) * kThreads * 8 + (n & 7);
+        if (i >= V) continue;
+        const float z = load_elem<DT>(row, i);
+        if (((__float_as_uint(z) >> 16) & 0x7FFFu) - kExpLow >= (uint32_t)kExps && z > -CUDART_INF_F) s[0] += exp(((double)z - (double)R) * beta);
+      }
+    }
+  }
+  return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
 // Weight max(p - q, 0) of an entry in fp64 (q of a logit that is NaN: the entry is not drawn); mass: p.
 __device__ __forceinline__ double exact_weight(const DrawRow &w, int kind, int i, float z, float y, double &mass) {
   mass = exp(((double)z - (double)w.R) * w.beta - w.lnZ);
@@ -827,7 +868,11 @@ __device__ __forceinline__ Lead lead_of_warp(Lead l) {
 }
 
 struct DrawShared {
-  float gumbel[kScoresKept], score[kScoresKept];  // of the first blocks: variates, and upper bounds of the scores under p
+  float gumbel[kScoresKept];  // of the first blocks: variates
+  union {
+    float score[kScoresKept];  // and upper bounds of the scores under p
+    double exps[2 * kExps + 1];  // while a row is summed in fp64, and no score is needed
+  };
   Lead lead[kWarps], all;
   Exact exact[kWarps];
   double sum[2 * kWarps];
@@ -871,7 +916,7 @@ __global__ void __launch_bounds__(kThreads, CTAS) draw_kernel(const __grid_const
   const int first = p.first[b];
   int a = first < len ? first : len;
   const int64_t r0 = b * (p.drafts + 1);
-  auto exact_total = [&](const char *row, float R) { return block_sum(exact_terms<DT>(row, p.V, R, tau, tid, kThreads), sh.sum); };
+  auto exact_total = [&](const char *row, float R) { return block_sum(exact_terms<DT>(row, p.V, R, tau, sh.exps), sh.sum); };
   bool near = false;
   for (int j = tid; j < a; j += kThreads) near |= p.rows[r0 + j].state == kNear;
   VerifyRow rec = p.rows[r0 + a];
@@ -974,9 +1019,12 @@ __global__ void __launch_bounds__(kThreads, CTAS) draw_kernel(const __grid_const
   int tok = -1;
   if (sure && draw_in<DT>(w, w.kind, lead.lo_b, u_in, false, sh.sum, tok)) return finish(tok);
 
-  // ---- the normaliser in fp64, and with it the blocks that the bounds did not exclude; where nothing is left of p - q, from p
-  w.lnZ = log(exact_total(w.z, w.R));
-  lnz = (float)w.lnZ;
+  // ---- the blocks that the bounds did not exclude, in fp64; where nothing is left of p - q, from p.  The normaliser counts only beside a q that is not in
+  // proportion to p.
+  if (w.kind == kDistribution) {
+    w.lnZ = log(exact_total(w.z, w.R));
+    lnz = (float)w.lnZ;
+  }
   if (sure) {
     draw_in<DT>(w, w.kind, lead.lo_b, u_in, true, sh.sum, tok);
     return finish(tok);
