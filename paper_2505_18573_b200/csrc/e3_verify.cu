@@ -14,7 +14,7 @@
 // block's own score: three or four of them as a rule.  (Reading the row and the draft's row again, 512 x 151,936, took 164 us.)
 //
 // Two tokens are the same only if every comparison falls the same way, so each is made with a bound on the error of fp32 sums; what the
-// bound does not settle (a few in 10,000) is taken again in fp64.
+// bound does not settle (one sequence in about 1,000) is taken again in fp64.
 #include "e3_rows_device.cuh"
 
 #include <mutex>
@@ -390,8 +390,8 @@ __device__ __noinline__ void decide(const VerifyParams &p, int64_t r, int64_t b,
   }
 }
 
-// Bound by the exponentials' and the other instructions' issue (70 for a lane's eight logits; 512 sequences of 3 drafts, 151,936 bf16: issue 71 %, DRAM 41 %,
-// 97 us for 332 MB) and by latency: a CTA of four warps takes a part of up to
+// Bound by the exponentials' and the other instructions' issue (70 for a lane's eight logits; 512 sequences of 3 drafts, 151,936 bf16: issue 70 %, DRAM 48 %,
+// 91 us for 356 MB) and by latency: a CTA of four warps takes a part of up to
 // 24 KB, all of it under way at once, eight of them an SM.  Larger CTAs wait longer for their last warp and for the decision; warps that run on from part
 // to part without a barrier (three steps of 2 KB under way each) were slower for their fences and read a third more rows that were not wanted.
 template <int DT>
