@@ -14,7 +14,7 @@
 // block's own score: three or four of them as a rule.  (Reading the row and the draft's row again, 512 x 151,936, took 164 us.)
 //
 // Two tokens are the same only if every comparison falls the same way, so each is made with a bound on the error of fp32 sums; what the
-// bound does not settle (one sequence in about 1,000) is taken again in fp64.
+// bound does not settle (one sequence in about 1,000) is taken again in fp64, first with the normaliser at hand.
 #include "e3_rows_device.cuh"
 
 #include <mutex>
@@ -730,12 +730,17 @@ __device__ __noinline__ double exact_terms(const char *row, int V, float R, floa
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-// Weight max(p - q, 0) of an entry in fp64 (q of a logit that is NaN: the entry is not drawn); mass: p.
-__device__ __forceinline__ double exact_weight(const DrawRow &w, int kind, int i, float z, float y, double &mass) {
-  mass = exp(((double)z - (double)w.R) * w.beta - w.lnZ);
+// Weight max(p - q, 0) of an entry in fp64 (q of a logit that is NaN: the entry is not drawn).  open: by how much the weight may turn otherwise than in
+// proportion where Z is known to kZError, in units of that: a weight p (1 + e) - q is (1 + e) (p - q) and e q more, and one within e p of 0 may come or go.
+__device__ __forceinline__ double exact_weight(const DrawRow &w, int kind, int i, float z, float y, double &open) {
+  const double mass = exp(((double)z - (double)w.R) * w.beta - w.lnZ);
+  open = 0.0;
   if (kind == kNoDraft) return mass;
   if (kind == kOneHot) return i == w.d ? 0.0 : mass;
-  return fmax(mass - exp(((double)y - (double)w.y_d) * w.beta_d + w.lnq), 0.0);
+  const double q = exp(((double)y - (double)w.y_d) * w.beta_d + w.lnq), r = mass - q;
+  if (r > 0.0) open = q;
+  if (fabs(r) <= 2.0 * kZError * mass) open += 2.0 * mass;
+  return r > 0.0 ? r : 0.0;
 }
 
 // Draw inside block b by the CTA, an entry a thread (a warp with eight entries a lane took 8 us: the exponentials are in fp64).  False: the fp32
@@ -744,36 +749,36 @@ template <int DT>
 __device__ __noinline__ bool draw_in(const DrawRow &w, int kind, int b, double u, bool exact, double *sh /* [2 * warps] */, int &tok) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, i = b * E3_SAMPLE_BLOCK + tid;
   static_assert(kThreads == E3_SAMPLE_BLOCK, "an entry a thread");
-  double r = 0.0, mass = 0.0;
-  if (i < w.V) r = exact_weight(w, kind, i, load_elem<DT>(w.z, i), kind == kDistribution ? load_elem<DT>(w.y, i) : 0.f, mass);
+  double r = 0.0, open = 0.0;
+  if (i < w.V) r = exact_weight(w, kind, i, load_elem<DT>(w.z, i), kind == kDistribution ? load_elem<DT>(w.y, i) : 0.f, open);
   double sum = r;  // of the warp's entries up to this one
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const double up = __shfl_up_sync(kAll, sum, o);
     if (lane >= o) sum += up;
-    mass += __shfl_xor_sync(kAll, mass, o);
+    open += __shfl_xor_sync(kAll, open, o);
   }
   __syncthreads();
   if (lane == 31) {
     sh[warp] = sum;
-    sh[kWarps + warp] = mass;
+    sh[kWarps + warp] = open;
   }
   __syncthreads();
   double total = 0.0;
-  mass = 0.0;
+  open = 0.0;
 #pragma unroll
   for (int k = 0; k < kWarps; ++k) {
     if (k < warp) sum += sh[k];
     total += sh[k];
-    mass += sh[kWarps + k];
+    open += sh[kWarps + k];
   }
-  const double t = u * total, margin = exact || kind != kDistribution ? 0.0 : kZError * mass;
-  const bool near = i < w.V && margin > 0.0 && fabs(sum - t) <= margin;
+  const double t = u * total, margin = exact || kind != kDistribution ? 0.0 : 1.01 * kZError * open;
+  const bool close = i < w.V && margin > 0.0 && fabs(sum - t) <= margin;
   int first = sum > t && r > 0.0 ? i : INT_MAX, last = r > 0.0 ? i : -1;
   first = __reduce_min_sync(kAll, first);
   last = __reduce_max_sync(kAll, last);
   int *const ints = reinterpret_cast<int *>(sh);
-  const bool open = __syncthreads_or(near);  // (and the sums have been read)
+  const bool undecided = __syncthreads_or(close);  // (and the sums have been read)
   if (lane == 0) {
     ints[2 * warp] = first;
     ints[2 * warp + 1] = last;
@@ -786,7 +791,7 @@ __device__ __noinline__ bool draw_in(const DrawRow &w, int kind, int b, double u
   }
   __syncthreads();
   tok = first != INT_MAX ? first : last;
-  return !open && tok >= 0;
+  return !undecided && tok >= 0;
 }
 
 // Score of block b under p, but for the constant -ln Z (natural logarithms): ln of its sum plus its Gumbel variate.
@@ -832,20 +837,53 @@ struct Exact {
   double y;
   int b;
 };
-// Exact score of block b with the weights of `kind`, by a warp; false: weight 0.
+// The two leading ones of scores that are known but for a bound.
+struct Near {
+  double lo, hi1, hi2;
+  int lo_b, hi_b;
+};
+__device__ __forceinline__ Near no_near() { return Near{-CUDART_INF, -CUDART_INF, -CUDART_INF, INT_MAX, INT_MAX}; }
+__device__ __forceinline__ void merge(Near &a, const Near &o) {
+  if (o.lo > a.lo) {
+    a.lo = o.lo;
+    a.lo_b = o.lo_b;
+  }
+  if (o.hi1 > a.hi1) {
+    a.hi2 = fmax(a.hi1, o.hi2);
+    a.hi1 = o.hi1;
+    a.hi_b = o.hi_b;
+  } else {
+    a.hi2 = fmax(a.hi2, o.hi1);
+  }
+}
+// Score of block b with the weights of `kind` in fp64, by a warp; false: weight 0.  off: what an error of kZError in Z may move it against other blocks'.  A
+// block's sum r turns into r (1 + e) + e g with |g| at most the sum of `open`, and ln(1 + e) is common to all blocks.
 template <int DT>
-__device__ __noinline__ bool exact_score_of(const DrawRow &w, int kind, int b, double u, double &y) {
+__device__ __noinline__ bool exact_score_of(const DrawRow &w, int kind, int b, double u, double &y, double &off) {
   const int lane = threadIdx.x & 31, i0 = b * E3_SAMPLE_BLOCK + lane * 8;
   const Eight<DT> z = load_eight<DT>(w.z, w.V, i0);
   Eight<DT> d = z;
   if (kind == kDistribution) d = load_eight<DT>(w.y, w.V, i0);
-  double r = 0.0, m;
+  double r = 0.0, g = 0.0, open;
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
-    if (i0 + k < w.V) r += exact_weight(w, kind, i0 + k, entry<DT>(z, k), entry<DT>(d, k), m);
+  for (int k = 0; k < 8; ++k) {
+    if (i0 + k < w.V) {
+      r += exact_weight(w, kind, i0 + k, entry<DT>(z, k), entry<DT>(d, k), open);
+      g += open;
+    }
+  }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) r += __shfl_xor_sync(kAll, r, o);
-  if (!(r > 0.0)) return false;
+  for (int o = 16; o > 0; o >>= 1) {
+    r += __shfl_xor_sync(kAll, r, o);
+    g += __shfl_xor_sync(kAll, g, o);
+  }
+  off = 0.0;
+  if (!(r > 0.0)) {
+    off = g > 0.0 ? CUDART_INF : 0.0;
+    return false;
+  }
+  const double e = 1.01 * kZError * g / r, x = e + kZError;
+  off = x < 0.1 ? e + x * x + 1e-12 : CUDART_INF;  // (|ln(1 + x) - x| <= x^2)
   y = log(r) - log(-log(u));
   return true;
 }
@@ -874,7 +912,10 @@ struct DrawShared {
     double exps[2 * kExps + 1];  // while a row is summed in fp64, and no score is needed
   };
   Lead lead[kWarps], all;
-  Exact exact[kWarps];
+  union {
+    Exact exact[kWarps];
+    Near close[kWarps];
+  };
   double sum[2 * kWarps];
   int reached;  // score of p - q that some block reaches, encoded
 };
@@ -1016,35 +1057,58 @@ __global__ void __launch_bounds__(kThreads, CTAS) draw_kernel(const __grid_const
     lead = lead_of_cta(mine, sh);
   }
   const bool sure = lead.lo > -CUDART_INF_F && lead.hi_b == lead.lo_b && lead.lo > lead.hi2;
-  int tok = -1;
-  if (sure && draw_in<DT>(w, w.kind, lead.lo_b, u_in, false, sh.sum, tok)) return finish(tok);
+  int tok = -1, chosen = sure ? lead.lo_b : INT_MAX;
+  if (sure && draw_in<DT>(w, w.kind, chosen, u_in, false, sh.sum, tok)) return finish(tok);
 
-  // ---- the blocks that the bounds did not exclude, in fp64; where nothing is left of p - q, from p.  The normaliser counts only beside a q that is not in
-  // proportion to p.
-  if (w.kind == kDistribution) {
-    w.lnZ = log(exact_total(w.z, w.R));
-    lnz = (float)w.lnZ;
-  }
-  if (sure) {
-    draw_in<DT>(w, w.kind, lead.lo_b, u_in, true, sh.sum, tok);
-    return finish(tok);
-  }
-  int kind = w.kind;
-  float floor = kind == kNoDraft ? reached_p - 1e-5f : lead.lo;  // a score that some block reaches (ln Z is in it)
-  for (int round = 0; round < 2; ++round) {
-    Exact e = {0.0, INT_MAX};
+  // Visits the blocks whose scores of p reach `floor`, a warp each.
+  auto visit = [&](float floor, auto &&with) {
     for (int i0 = warp * 32; i0 < p.blocks; i0 += kThreads) {
       Score most = {-CUDART_INF_F, 0.f};
       if (i0 + lane < p.blocks) most = score_at(i0 + lane, __ldcg(sums + i0 + lane));
       const float hi = most.y + most.off - lnz + 1e-5f;
       uint32_t open = __ballot_sync(kAll, hi > -CUDART_INF_F && hi >= floor);
       while (open != 0u) {
-        const int i = i0 + __ffs((int)open) - 1;
+        with(i0 + __ffs((int)open) - 1);
         open &= open - 1u;
-        double y;
-        if (exact_score_of<DT>(w, kind, i, u[i], y)) merge(e, Exact{y, i});
       }
     }
+  };
+  if (w.kind == kDistribution) {
+    // ---- two blocks that fp32 leaves open: their scores in fp64 with the normaliser at hand, as a rule that settles them
+    if (!sure) {
+      Near mine = no_near();
+      visit(lead.lo, [&](int i) {
+        double y, off;
+        const bool any = exact_score_of<DT>(w, kDistribution, i, u[i], y, off);
+        if (any || off > 0.0) merge(mine, any ? Near{y - off, y + off, -CUDART_INF, i, i} : Near{-CUDART_INF, CUDART_INF, -CUDART_INF, INT_MAX, i});
+      });
+      __syncthreads();
+      if (lane == 0) sh.close[warp] = mine;
+      __syncthreads();
+      mine = sh.close[0];
+      for (int i = 1; i < kWarps; ++i) merge(mine, sh.close[i]);
+      if (mine.lo > -CUDART_INF && mine.lo_b == mine.hi_b && mine.lo > mine.hi2) {
+        chosen = mine.lo_b;
+        if (draw_in<DT>(w, kDistribution, chosen, u_in, false, sh.sum, tok)) return finish(tok);
+      }
+    }
+    // ---- the normaliser in fp64: it counts only beside a q that is not in proportion to p
+    w.lnZ = log(exact_total(w.z, w.R));
+    lnz = (float)w.lnZ;
+    if (chosen != INT_MAX) {
+      draw_in<DT>(w, kDistribution, chosen, u_in, true, sh.sum, tok);
+      return finish(tok);
+    }
+  }
+  // ---- the blocks that the bounds did not exclude, exactly; where nothing is left of p - q, from p
+  int kind = w.kind;
+  float floor = kind == kNoDraft ? reached_p - 1e-5f : lead.lo;  // a score that some block reaches (ln Z is in it)
+  for (int round = 0; round < 2; ++round) {
+    Exact e = {0.0, INT_MAX};
+    visit(floor, [&](int i) {
+      double y, off;
+      if (exact_score_of<DT>(w, kind, i, u[i], y, off)) merge(e, Exact{y, i});
+    });
     __syncthreads();
     if (lane == 0) sh.exact[warp] = e;
     __syncthreads();

@@ -263,9 +263,10 @@ def test_uniforms_next_to_the_ratio(e3, sign):
         s.check(e3)
 
 
-@pytest.mark.parametrize("sign", [-1, 1])
-def test_blocks_and_entries_next_to_each_other(e3, sign):
-    """Two leading blocks, and a prefix sum and the uniform, closer than sums in fp32 can tell."""
+# gaps that need the row's normaliser in fp64, that scores in fp64 settle without it, and that fp32 settles
+@pytest.mark.parametrize("gap", [s * g for g in (1e-9, 1e-7, 1e-6, 1e-5, 1e-4) for s in (-1, 1)])
+def test_blocks_and_entries_next_to_each_other(e3, gap):
+    """Two leading blocks, and a prefix sum and the uniform, close to each other."""
     for model in (True, False):
         s = Batch(10, 12, 1, 2800, model=model)
         s.uniforms[:, 0] = 1 - 1e-12  # refused nearly everywhere
@@ -287,11 +288,11 @@ def test_blocks_and_entries_next_to_each_other(e3, sign):
             score = np.log(sums) - np.log(-np.log(u[b, 1:-1]))
             first, second = np.argsort(-score)[:2]
             if b % 2 == 0:  # the second block's uniform puts it next to the first
-                s.uniforms[b, 1 + second] = math.exp(-math.exp(-(score[first] + sign * 1e-9 - math.log(sums[second]))))
+                s.uniforms[b, 1 + second] = math.exp(-math.exp(-(score[first] + gap - math.log(sums[second]))))
             else:  # the draw inside the block next to a border
                 part = full[first * BLOCK:(first + 1) * BLOCK]
                 prefix = np.cumsum(part) / part.sum()
-                s.uniforms[b, -1] = min(max(prefix[100] * (1 + sign * 1e-9), 0.0), 1 - 1e-9)
+                s.uniforms[b, -1] = min(max(prefix[100] * (1 + gap), 0.0), 1 - 1e-9)
         s.check(e3)
 
 
