@@ -10,7 +10,8 @@
 //   - More rows: 128 of the hidden states' rows are M and 256 vocabulary entries N.  A lane has a row, so that its scale is one register and the
 //     sums cost one multiply-add per entry and block and nothing else (with the other form's scales, four bytes per entry and block from shared
 //     memory, a block of 128 x 256 x 128 took 2,200 cycles, the products 512).  Bound by the tensor memory, where the products of a block (512 cycles) and
-//     the reads of its sums (256) take turns: 740 to 800 cycles a block; 512 rows, a table of 151,936 x 2,048: 169 us, 1.9 PFLOP/s.
+//     the reads of its sums (256) take turns: 740 to 800 cycles a block; 512 rows, a table of 151,936 x 2,048: 169 us, 1.9 PFLOP/s
+//     (190 to 200 in runs of seconds, in which the power limit holds the clock at 1.5 GHz).
 //
 // Every wait is bounded: one that runs out marks the call's status word, and the CTA's unfinished logits read NaN.
 #include "e3_rows_device.cuh"
