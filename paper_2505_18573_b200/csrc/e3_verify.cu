@@ -1060,13 +1060,14 @@ __global__ void __launch_bounds__(kThreads, CTAS) draw_kernel(const __grid_const
   int tok = -1, chosen = sure ? lead.lo_b : INT_MAX;
   if (sure && draw_in<DT>(w, w.kind, chosen, u_in, false, sh.sum, tok)) return finish(tok);
 
-  // Visits the blocks whose scores of p reach `floor`, a warp each.
+  // Visits the blocks whose scores of p reach `floor`, a warp each; all blocks where nothing is known to be reached (-inf: a block's score is that too
+  // where its uniform is 0, and what fp32 does not hold may have weight).
   auto visit = [&](float floor, auto &&with) {
     for (int i0 = warp * 32; i0 < p.blocks; i0 += kThreads) {
       Score most = {-CUDART_INF_F, 0.f};
       if (i0 + lane < p.blocks) most = score_at(i0 + lane, __ldcg(sums + i0 + lane));
       const float hi = most.y + most.off - lnz + 1e-5f;
-      uint32_t open = __ballot_sync(kAll, hi > -CUDART_INF_F && hi >= floor);
+      uint32_t open = __ballot_sync(kAll, i0 + lane < p.blocks && hi >= floor);
       while (open != 0u) {
         with(i0 + __ffs((int)open) - 1);
         open &= open - 1u;
