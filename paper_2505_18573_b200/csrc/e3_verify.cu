@@ -1014,9 +1014,10 @@ __global__ void __launch_bounds__(kThreads, CTAS) draw_kernel(const __grid_const
     insert(lead, y.y - y.off, y.y + y.off, i);
   }
   w.beta = 1.0 / (double)tau; w.c = __fdiv_rn(kLog2e, tau); w.nz = -(float)(rec.lnZ * (1.0 / kLn2));
+  // (the normaliser that the decision had, on every way here: which way a draw takes may hang on which warp was first to reach a score)
   auto finish = [&](int tok) {
     if (tok < 0) return write(-1, CUDART_NAN_F, CUDART_NAN_F);
-    if (tid == 0) write(tok, (float)(((double)load_elem<DT>(w.z, tok) - (double)w.R) * w.beta - w.lnZ), rec.ent);
+    if (tid == 0) write(tok, (float)(((double)load_elem<DT>(w.z, tok) - (double)w.R) * w.beta - rec.lnZ), rec.ent);
   };
   lead = lead_of_cta(lead_of_warp(lead), sh);
   if (lead.bad != 0 || !usable_uniform(u_in)) return write(-1, CUDART_NAN_F, CUDART_NAN_F);

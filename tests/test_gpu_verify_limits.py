@@ -120,3 +120,13 @@ def test_greedy_sequences_look_at_no_uniforms_of_the_draw(e3, dtype):
     tok, kept, logp, ent = s.call(e3)
     assert bool((tok == -1).all()) and not kept.any() and bool(logp[:, 0].isnan().all()) and bool(ent[:, 0].isnan().all())
     assert host(tok).shape == (12, 3)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_log_probabilities_hang_on_the_row_alone(e3, dtype):
+    """However near the draw's other candidates come: the same bits whether fp32 settles it or the row's normaliser is taken in fp64 for it."""
+    s = Batch(7, 60, 1, 256, dtype)
+    s.uniforms[:, 1] = 0.5
+    want = s.call(e3)
+    s.uniforms[:, 1] = 0.0  # (one block, whose score fp32 cannot tell from others')
+    assert all(torch.equal(x, y) for x, y in zip(s.call(e3), want))
