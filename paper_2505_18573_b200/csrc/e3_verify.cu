@@ -553,7 +553,7 @@ __global__ void __launch_bounds__(kRowThreads, kHeld) verify_rows_kernel(const _
       }
       const float sum = warp_sums(z);
       const int k = k0 + lane / (32 / kStep);
-      if (lane % (32 / kStep) == 0 && k < count) sums[k] = make_float2(sound ? sum * f : sum, s.R > -CUDART_INF_F ? s.R : 0.f);
+      if (lane % (32 / kStep) == 0 && k < count) sums[k] = make_float2(sound ? sum * f : sum, s.R);  // (-inf: nothing but -inf so far)
     }
   }
   // ---- the part's result, joined in a fixed order
@@ -795,12 +795,14 @@ __device__ __noinline__ bool draw_in(const DrawRow &w, int kind, int b, double u
 }
 
 // Score of block b under p, but for the constant -ln Z (natural logarithms): ln of its sum plus its Gumbel variate.
+constexpr float kFlushed = 0x1p-118f;  // what a block's 256 terms may lack in fp32: each that is below 2^-126 reads 0
 struct Score {
-  float y, off;  // value, bound on its error
+  float y, off, hi;  // value, bound on its error but for terms that read 0, upper bound
 };
 __device__ __forceinline__ Score score_of_p(const float2 &s, float gumbel, float R, float tau) {
-  const float x = s.x > 0.f ? __fdiv_rn(fmaxf(s.y - R, -kFarBelow), tau) : -CUDART_INF_F, y = logf(s.x) + x + gumbel;
-  return Score{y, 1.2e-5f + 2e-6f * (fabsf(x) < 1e3f ? fabsf(x) : 1e3f)};
+  const float x = __fdiv_rn(fmaxf(s.y - R, -kFarBelow), tau), y = logf(s.x) + x + gumbel;
+  const float off = 1.2e-5f + 2e-6f * (fabsf(x) < 1e3f ? fabsf(x) : 1e3f);
+  return Score{y, off, (s.x > 0x1p-94f ? y : logf(s.x + kFlushed) + x + gumbel) + off};
 }
 
 // Score of a block with weights p - q, with bounds, by a warp.
@@ -826,7 +828,7 @@ __device__ __forceinline__ void score_block(const DrawRow &w, int b, float gumbe
     r += __shfl_xor_sync(kAll, r, o);
     s += __shfl_xor_sync(kAll, s, o);
   }
-  const float off = s * (kSumError + kSumErrorPerBit * (fmaxf(-lg2f(s), 0.f) + 2.f * fabsf(w.nq))) + 1e-37f;
+  const float off = s * (kSumError + kSumErrorPerBit * (fmaxf(-lg2f(fmaxf(s, kFlushed)), 0.f) + 2.f * fabsf(w.nq))) + 2.f * kFlushed;
   hi = logf(r + off) + gumbel;
   lo = r > off ? logf(r - off) + gumbel : -CUDART_INF_F;
   hi += 6e-6f + 5e-7f * fabsf(hi);
@@ -1010,8 +1012,8 @@ __global__ void __launch_bounds__(kThreads, CTAS) draw_kernel(const __grid_const
     if (i + kThreads < p.blocks) sum = __ldcg(sums + i + kThreads);
     const Score y = score_at(i, s);
     lead.bad |= y.y != y.y;
-    if (i < kScoresKept) sh.score[i] = y.y + y.off;
-    insert(lead, y.y - y.off, y.y + y.off, i);
+    if (i < kScoresKept) sh.score[i] = y.hi;
+    insert(lead, y.y - y.off, y.hi, i);
   }
   w.beta = 1.0 / (double)tau; w.c = __fdiv_rn(kLog2e, tau); w.nz = -(float)(rec.lnZ * (1.0 / kLn2));
   // (the normaliser that the decision had, on every way here: which way a draw takes may hang on which warp was first to reach a score)
@@ -1027,8 +1029,7 @@ __global__ void __launch_bounds__(kThreads, CTAS) draw_kernel(const __grid_const
     // weights p - q: those blocks whose scores of p reach the best known score of p - q
     auto bound = [&](int i) {
       if (i < kScoresKept) return sh.score[i];
-      const Score y = score_at(i, __ldcg(sums + i));
-      return y.y + y.off;
+      return score_at(i, __ldcg(sums + i)).hi;
     };
     Lead mine = no_lead();
     float last = CUDART_INF_F;  // a warp takes its blocks in the order of their scores of p, highest first
@@ -1065,9 +1066,8 @@ __global__ void __launch_bounds__(kThreads, CTAS) draw_kernel(const __grid_const
   // where its uniform is 0, and what fp32 does not hold may have weight).
   auto visit = [&](float floor, auto &&with) {
     for (int i0 = warp * 32; i0 < p.blocks; i0 += kThreads) {
-      Score most = {-CUDART_INF_F, 0.f};
-      if (i0 + lane < p.blocks) most = score_at(i0 + lane, __ldcg(sums + i0 + lane));
-      const float hi = most.y + most.off - lnz + 1e-5f;
+      float hi = -CUDART_INF_F;
+      if (i0 + lane < p.blocks) hi = score_at(i0 + lane, __ldcg(sums + i0 + lane)).hi - lnz + 1e-5f;
       uint32_t open = __ballot_sync(kAll, i0 + lane < p.blocks && hi >= floor);
       while (open != 0u) {
         with(i0 + __ffs((int)open) - 1);

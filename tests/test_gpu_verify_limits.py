@@ -110,6 +110,26 @@ def test_what_is_left_is_less_than_fp32_holds(e3, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("alone", [-83.0, -60.0, -90.0])
+def test_weights_that_fp32_holds_beside_weights_that_it_does_not(e3, dtype, alone):
+    """Nothing left at the draft; one entry of exp(alone) in a block, 256 of exp(-88) in another: fp32 holds exp(-83), but neither exp(-88) nor its sum's terms."""
+    n, V = 12, 6 * BLOCK
+    s = Batch(8, n, 1, V, dtype)
+    z = torch.full((n, 2, V), -INF, device="cuda")
+    z[:, :, 5 * BLOCK + 3], z[:, :, BLOCK + 9], z[:, :, 4 * BLOCK:5 * BLOCK] = 0.0, alone, -88.0  # (0 and -88 under one reference)
+    s.logits = z.view(2 * n, V).to(dtype)
+    y = torch.full((n, V), -INF, device="cuda")
+    y[:, 5 * BLOCK + 3] = 0.0
+    s.draft_logits, s.draft_tok, s.temps = y.to(dtype), torch.full_like(s.draft_tok, 5 * BLOCK + 3), torch.ones_like(s.temps)
+    s.draft_temps, s.draft_logp = s.temps, torch.full((n, 1), 1e-3, device="cuda")
+    s.uniforms[:, 0], s.uniforms[:, 2], s.uniforms[:, 5] = 1 - 1e-9, 0.5, 0.5
+    tok, kept, _, _ = s.call(e3)
+    want = reference(s)
+    assert not kept.any() and np.array_equal(tok.cpu().numpy(), want[0])
+    assert bool((tok[:, 0] // BLOCK == (1 if alone == -60.0 else 4)).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_greedy_sequences_look_at_no_uniforms_of_the_draw(e3, dtype):
     """At tau = 0 the token behind the kept drafts is the arg-max: of the uniforms only u_j has to lie in [0, 1)."""
     s = Batch(6, 12, 2, 900, dtype, greedy=1.0)
