@@ -32,10 +32,13 @@ constexpr float kFarBelow = 3e38f;    // distances below the largest logit are n
 constexpr float kFarFrom = 0x1p20f;    // |R log2(e) / tau| from which t is taken from z - R
 constexpr float kSoundSum = 0x1p20f;   // a lane's sum from which a higher reference is taken
 constexpr int kScoresKept = 2048;  // blocks whose scores of p stay in shared memory
-// Relative error of sums of p and q over a block in fp32 (2^t: 2^-22 and the rounding of t) and through Z, and of Z.
-constexpr float kSumError = 5e-6f;
+// Relative error of Z, whatever V is: more than 32 parts are added in fp64 (`decide`), so what adds up is a part's own.  A term: 2^t 2^-22, and t's rounding,
+// two steps of 2^-24 of |t| < 32 bits (further down lies no mass), 1.6e-6; at most 28 sums one after the other, 2^-24 each, 1.7e-6; 2^-22 and three steps for
+// each move to another reference, five in a row of steps, the CTA's and the row's, 2.6e-6.
+constexpr double kZError = 6e-6;
+// Relative error of sums of p and q over a block in fp32 (2^t: 2^-22, and 13 sums) and through Z.
+constexpr float kSumError = 8e-6f;
 constexpr float kSumErrorPerBit = 1.5e-7f;  // per factor of two by which the sum, or the draft's own q, lies below 1 (rounding of t)
-constexpr double kZError = 3e-6;  // (sums of at most forty roundings one after the other, 2^-24 each, 2^t: 2^-22)
 
 enum : int { kKept = 0, kRefused = 1, kInvalid = 2, kNear = 3 };  // kNear: u q is closer to p than Z is known; kept for the time being
 
@@ -171,16 +174,6 @@ __device__ __forceinline__ float most_of(const uint4 &v) {
 struct Sums {
   float R, Z, W;
 };
-// Joins two sums; either may be empty (R = -inf, Z = 0).
-__device__ __forceinline__ void join(Sums &a, float R, float Z, float W, float c) {
-  const float m = fmaxf(a.R, R);
-  if (m == -CUDART_INF_F) return;
-  const float da = fmaxf((a.R - m) * c, -kFarBelow), db = fmaxf((R - m) * c, -kFarBelow);
-  const float fa = a.Z > 0.f ? ex2f(da) : 0.f, fb = Z > 0.f ? ex2f(db) : 0.f;
-  a.W = (fa > 0.f ? fa * fmaf(da, a.Z, a.W) : 0.f) + (fb > 0.f ? fb * fmaf(db, Z, W) : 0.f);
-  a.Z = fa * a.Z + fb * Z;
-  a.R = m;
-}
 // Joins the sums of the first N lanes (empty ones: R = -inf, Z = 0) in a fixed order, for all of these lanes.
 template <int N>
 __device__ __forceinline__ void join_lanes(Sums &s, float c) {
@@ -345,42 +338,64 @@ __device__ __noinline__ void decide(const VerifyParams &p, int64_t r, int64_t b,
     u = p.uniforms[b * p.u_stride + j];
     if (d.kind != kNoDraft) zd = load_elem<DT>(p.logits + r * p.row_bytes, d.tok);
   }
-  Sums s = {-CUDART_INF_F, 0.f, 0.f};
+  float R = -CUDART_INF_F;
+  float Z = 0.f, W = 0.f;
   int best = INT_MAX;
   bool bad = false;
-  for (int i = lane; i < p.n_parts; i += 32) {  // (written by other SMs: from L2)
-    const int4 *const src = reinterpret_cast<const int4 *>(p.parts + r * p.n_parts + i);
-    const int4 x = __ldcg(src), y = __ldcg(src + 1);
-    const float R = __int_as_float(x.x);
+  const int4 *const parts = reinterpret_cast<const int4 *>(p.parts + r * p.n_parts);  // (written by other SMs: from L2)
+  int4 first = make_int4(0, 0, 0, 0);
+  for (int i = lane; i < p.n_parts; i += 32) {
+    const int4 x = __ldcg(parts + 2 * i);
+    if (i == lane) first = x;
+    const float top = __int_as_float(x.x);
     bad |= x.w != 0;
     if (greedy) {
-      if (R > s.R || (R == s.R && y.x < best)) {
-        s.R = R;
-        best = y.x;
-      }
-    } else {
-      join(s, R, __int_as_float(x.y), __int_as_float(x.z), c);
+      const int at = __ldcg(&parts[2 * i + 1].x);
+      if (top > R || (top == R && at < best)) best = at;
     }
+    R = fmaxf(R, top);
   }
   bad = __any_sync(kAll, bad);
-  if (greedy) best_of_warp(s.R, best);
-  else join_lanes<32>(s, c);
+  if (greedy) {
+    best_of_warp(R, best);
+  } else {  // each part moves to the row's reference once, and a lane adds its parts in fp64: no error grows with their number
+    R = dec_float(__reduce_max_sync(kAll, enc_float(R)));
+    auto add = [&](const int4 &x, auto &to_Z, auto &to_W) {
+      using T = std::remove_reference_t<decltype(to_Z)>;
+      const float t = fmaxf((__int_as_float(x.x) - R) * c, -kFarBelow), z = __int_as_float(x.y) * ex2f(t);
+      if (!(z > 0.f)) return;
+      to_Z += (T)z;
+      to_W += (T)fmaf(t, z, ex2f(t) * __int_as_float(x.z));
+    };
+    add(first, Z, W);
+    if (p.n_parts > 32) {
+      double Z_on = Z, W_on = W;
+      for (int i = lane + 32; i < p.n_parts; i += 32) add(__ldcg(parts + 2 * i), Z_on, W_on);
+      Z = (float)Z_on;
+      W = (float)W_on;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      Z += __shfl_xor_sync(kAll, Z, o);
+      W += __shfl_xor_sync(kAll, W, o);
+    }
+  }
   if (lane != 0) return;
-  VerifyRow w = {0.0, d.lnq, s.R, 0.f, 0.f, d.y, kRefused, best, d.kind, d.tok};
-  if (bad || !(s.R > -CUDART_INF_F) || (!greedy && !(s.Z > 0.f)) || !usable_uniform(u)) {
+  VerifyRow w = {0.0, d.lnq, R, 0.f, 0.f, d.y, kRefused, best, d.kind, d.tok};
+  if (bad || !(R > -CUDART_INF_F) || (!greedy && !(Z > 0.f)) || !usable_uniform(u)) {
     w.state = kInvalid;
   } else if (greedy) {
     if (d.kind != kNoDraft && d.tok == best && u * exp(d.lnq) < 1.0) w.state = kKept;
   } else {
     // c is log2(e) / tau rounded to fp32: that turns t by as much, and ln Z by the mean of t
-    const double beta = 1.0 / (double)tau, mean = (double)__fdiv_rn(s.W, s.Z) * kLn2, lnZ = log((double)s.Z);
+    const double beta = 1.0 / (double)tau, mean = (double)__fdiv_rn(W, Z) * kLn2, lnZ = log((double)Z);
     w.lnZ = lnZ + (beta / (kLn2 * (double)c) - 1.0) * mean;
     w.ent = (float)fmax(lnZ - mean, 0.0);
     if (d.kind != kNoDraft) {
-      const double lp = ((double)zd - (double)s.R) * beta - w.lnZ;
+      const double lp = ((double)zd - (double)R) * beta - w.lnZ;
       const double ratio = u * exp(d.lnq - lp);  // (a token of probability 0: infinity or, from u = 0, NaN)
       w.logp = (float)lp;
-      w.state = fabs(ratio - 1.0) < 2.0 * kZError ? kNear : (ratio < 1.0 ? kKept : kRefused);
+      w.state = fabs(ratio - 1.0) < 1.01 * kZError ? kNear : (ratio < 1.0 ? kKept : kRefused);
     }
   }
   p.rows[r] = w;
