@@ -32,6 +32,9 @@ constexpr float kFarBelow = 3e38f;    // distances below the largest logit are n
 constexpr float kFarFrom = 0x1p20f;    // |R log2(e) / tau| from which t is taken from z - R
 constexpr float kSoundSum = 0x1p20f;   // a lane's sum from which a higher reference is taken
 constexpr int kScoresKept = 2048;  // blocks whose scores of p stay in shared memory
+// Blocks that a warp takes in the order of their scores, each found by a look at all of them, which many blocks times long rows would make quadratic; where
+// that does not do (next to nothing is left of p - q), all that may lead are looked at one after the other.
+constexpr int kInOrder = 128;  // (all blocks of rows of 262,144)
 // Relative error of Z, whatever V is: more than 32 parts are added in fp64 (`decide`), so what adds up is a part's own.  A term: 2^t 2^-22, and t's rounding,
 // two steps of 2^-24 of |t| < 32 bits (further down lies no mass), 1.6e-6; at most 28 sums one after the other, 2^-24 each, 1.7e-6; 2^-22 and three steps for
 // each move to another reference, five in a row of steps, the CTA's and the row's, 2.6e-6.
@@ -1049,7 +1052,11 @@ __global__ void __launch_bounds__(kThreads, CTAS) draw_kernel(const __grid_const
     Lead mine = no_lead();
     float last = CUDART_INF_F;  // a warp takes its blocks in the order of their scores of p, highest first
     int last_b = -1;
-    for (;;) {
+    for (int taken = 0;; ++taken) {
+      if (taken == kInOrder) {
+        mine.bad = 1;  // unfinished
+        break;
+      }
       float most = -CUDART_INF_F;
       int at = INT_MAX;
       for (int i = warp * 32 + lane; i < p.blocks; i += kThreads) {
@@ -1073,7 +1080,7 @@ __global__ void __launch_bounds__(kThreads, CTAS) draw_kernel(const __grid_const
     }
     lead = lead_of_cta(mine, sh);
   }
-  const bool sure = lead.lo > -CUDART_INF_F && lead.hi_b == lead.lo_b && lead.lo > lead.hi2;
+  const bool sure = lead.bad == 0 && lead.lo > -CUDART_INF_F && lead.hi_b == lead.lo_b && lead.lo > lead.hi2;
   int tok = -1, chosen = sure ? lead.lo_b : INT_MAX;
   if (sure && draw_in<DT>(w, w.kind, chosen, u_in, false, sh.sum, tok)) return finish(tok);
 

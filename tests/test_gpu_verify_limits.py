@@ -150,3 +150,13 @@ def test_log_probabilities_hang_on_the_row_alone(e3, dtype):
     want = s.call(e3)
     s.uniforms[:, 1] = 0.0  # (one block, whose score fp32 cannot tell from others')
     assert all(torch.equal(x, y) for x, y in zip(s.call(e3), want))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("error", [1e-5, 1e-3, 0.05])
+def test_a_draft_almost_like_the_target(e3, dtype, error):
+    """So little is left of p - q that most blocks' scores of p reach the best score of that, more than are taken in their order."""
+    s = Batch(9, 4, 1, 400_000, dtype, error=error, sharp=0.2)
+    s.draft_logp = s.draft_logp + 1e-4
+    s.uniforms[:, 0] = 1 - 1e-9
+    s.check(e3)

@@ -1,5 +1,6 @@
-"""Verification of drafted tokens in rows far longer than a vocabulary: what decides there is as exact as elsewhere."""
+"""Verification of drafted tokens in rows far longer than a vocabulary: what decides there is as exact as elsewhere, and takes time in proportion."""
 import math
+import time
 
 import pytest
 import torch
@@ -41,3 +42,28 @@ def test_sums_over_a_billion_entries(e3):
                 assert abs(logp[b, 0].item() - want[b]) <= 1e-5 + abs(want[b]) * 2.0 ** -23
         del logits
     torch.cuda.empty_cache()
+
+
+def test_a_draft_like_the_target_in_a_long_row(e3):
+    """Nothing is left of p - q, in any of 524,288 blocks: each is looked at a few times (0.5 s), not once for every other (half a minute)."""
+    V, n, k = 1 << 27, 1, 1
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    logits = torch.randn((n * (k + 1), V), generator=g, device="cuda", dtype=torch.bfloat16)
+    tok = torch.full((n, k), 1000, device="cuda", dtype=torch.int32)
+    z = logits[0].double()
+    logp = (z[1000] - z.logsumexp(0)).float().view(1, 1) + 1e-3  # q = 1.001 p
+    u = torch.rand((n, k + V // BLOCK + 1), generator=g, device="cuda", dtype=torch.float64)
+    u[:, 0] = 1 - 1e-9
+    torch.cuda.synchronize()
+    begin = time.perf_counter()
+    out, kept, _, _ = e3.e3_verify_drafts(logits, torch.ones(n, device="cuda"), tok, u, draft_logits=logits[:1], draft_logp=logp)
+    torch.cuda.synchronize()
+    assert time.perf_counter() - begin < 4.0
+    assert kept.item() == 0
+    # nothing left: the draw is from p
+    sums = torch.exp(z.view(-1, BLOCK) - z.max()).sum(1)
+    score = sums.log() - (-u[0, 1:-1].log()).log()
+    block = int(score.argmax())
+    prefix = torch.exp(z.view(-1, BLOCK)[block] - z.max()).cumsum(0)
+    assert out[0, 0].item() == block * BLOCK + int((prefix > u[0, -1] * prefix[-1]).int().argmax())
