@@ -214,7 +214,8 @@ E3_API e3_status e3_token_logp_entropy_backward(const void *logits, e3_dtype dt,
  * the drafts before position a are kept, and one more token is drawn at position a: from r = max(p_a - q_a, 0) where a draft was refused
  * (from p_a if nothing is left of r), from p_a behind the last draft.  The draw is that of E3_SAMPLER_BLOCK with the caller's uniforms: the block of
  * E3_SAMPLE_BLOCK entries with the largest ln(sum r_i) - ln(-ln v_b), then the first entry of it whose prefix sum exceeds w times its
- * sum; ties go to the lower index.  Comparisons that fp32 leaves open are made in fp64.
+ * sum; ties go to the lower index, also those of blocks whose v_b is 0 (score -inf, before blocks of which nothing is left).  Comparisons that fp32 leaves
+ * open are made in fp64.
  *
  *   logits        device, [n_seq * (max_draft + 1), V] with row_stride elements from row to row, position j of sequence b in row
  *                 b (max_draft + 1) + j; rows behind a sequence's last position are not read
@@ -232,8 +233,8 @@ E3_API e3_status e3_token_logp_entropy_backward(const void *logits, e3_dtype dt,
  *                 of p_j; 0 behind the drawn token
  *   workspace     e3_workspace_bytes(E3_CALL_VERIFY_DRAFTS, n_seq * (max_draft + 1), V, dt) bytes of device scratch
  * A position that is reached and whose row holds NaN or +inf or nothing but -inf, whose temperature is negative or not finite, or whose
- * uniform lies outside [0, 1) (of the block uniforms: any) ends the sequence: token -1, log-probability and entropy NaN.  n_seq * (max_draft + 1) < 2^26,
- * V < 2^31 - 2^16.
+ * u_j lies outside [0, 1) ends the sequence: token -1, log-probability and entropy NaN.  So does the draw where any v_b, or w, lies outside [0, 1); a greedy
+ * sequence draws nothing and looks at neither.  n_seq * (max_draft + 1) < 2^26, V < 2^31 - 2^16.
  */
 E3_API e3_status e3_verify_drafts(const void *logits, e3_dtype dt, int64_t n_seq, int64_t max_draft, int64_t V, int64_t row_stride,
                                   const float *temps, const int32_t *draft_tok, const int32_t *draft_len,
