@@ -915,8 +915,8 @@ extern "C" e3_status e3_project_vocab(const uint8_t *x, const float *x_scale, in
   using namespace e3;
   if (dt != E3_F32 && dt != E3_BF16) return E3_ERR_DTYPE;
   const int64_t most = int64_t(1) << 31, blocks = (D + kTileK - 1) / kTileK;
-  // (tiles may reach past the last row, coordinates are 32-bit)
-  if (rows < 0 || rows >= most - 256 || V < 1 || V >= most - kTileV || D < 1 || D >= most - kTileK || x_stride < D || w_stride < D ||
+  // (tiles of up to 256 may reach past the last row, entry or column, coordinates are 32-bit)
+  if (rows < 0 || rows >= most - 256 || V < 1 || V >= most - 256 || D < 1 || D >= most - 256 || x_stride < D || w_stride < D ||
       x_stride >= (int64_t(1) << 40) || w_stride >= (int64_t(1) << 40) || x_scale_stride < blocks || w_scale_stride < blocks || row_stride < V)
     return E3_ERR_INVALID_ARG;
   if (rows == 0) return E3_OK;
