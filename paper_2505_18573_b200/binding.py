@@ -4,6 +4,9 @@ Argument marshalling only: every step of the path runs in the CUDA library.  Dev
 ``torch`` CUDA tensors (used for their memory and stream, nothing else), pass raw pointers and
 sizes through the C ABI (in native code: ``_native``) and return the output tensors; the host calls go through ctypes.  There is
 no CPU fallback: if the library has not been built, or a tensor is not on a CUDA device, the call raises.
+
+Calls go to the current stream, or to ``stream``, which has to wait for the inputs as any other use of them there.  New outputs then
+belong to that stream's memory, and reads of them by the stream that is current at the call are waited for when they are dropped.
 """
 from __future__ import annotations
 

@@ -9,6 +9,7 @@
 #include <ATen/cuda/EmptyTensor.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty_like.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAException.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -144,13 +145,39 @@ struct Output {
 at::Tensor empty(at::IntArrayRef size, at::ScalarType dtype, at::Device device) {
   return at::detail::empty_cuda(size, dtype, device, std::nullopt);
 }
-Output output(PyObject *given, const char *name, bool make, at::IntArrayRef size, at::ScalarType dtype, at::Device device) {
+c10::cuda::CUDAStream torch_stream(cudaStream_t stream, at::Device device) {
+  return stream == nullptr || stream == cudaStreamLegacy ? c10::cuda::getDefaultCUDAStream(device.index())
+                                                         : c10::cuda::getStreamFromExternal(stream, device.index());
+}
+// The stream of a call.  New outputs belong to it, so that their memory is neither still in use by what the current stream does, nor given away before the
+// call has run; and the current stream is noted as one that uses them, so that dropping them waits for its reads.
+struct CallStream {
+  at::Device device;
+  cudaStream_t handle;
+  c10::cuda::CUDAStream current, call;
+  CallStream(PyObject *given, at::Device on)
+      : device(on), handle(stream_of(given)), current(c10::cuda::getCurrentCUDAStream(on.index())),
+        call(given == Py_None ? current : torch_stream(handle, on)) {}
+  operator cudaStream_t() const { return handle; }
+  template <class F>
+  at::Tensor make(F tensor) const {
+    if (call.stream() == current.stream()) return tensor();
+    const c10::cuda::CUDAStreamGuard guard(call);
+    at::Tensor t = tensor();
+    c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), current);
+    return t;
+  }
+  at::Tensor empty(at::IntArrayRef size, at::ScalarType dtype) const {
+    return make([&] { return ::empty(size, dtype, device); });
+  }
+};
+Output output(PyObject *given, const char *name, bool make, at::IntArrayRef size, at::ScalarType dtype, const CallStream &stream) {
   Output o;
   if (optional_tensor(given, name)) {
     o.object = given;
     o.any = true;
   } else if (make) {
-    o.made = empty(size, dtype, device);
+    o.made = stream.empty(size, dtype);
     o.any = true;
   }
   return o;
@@ -182,9 +209,7 @@ std::map<Key, at::Tensor> *g_kept = new std::map<Key, at::Tensor>();  // used wi
 std::mutex g_launch_lock;                                             // a call's kernels go to the stream together
 
 at::Tensor buffer_on(cudaStream_t stream, size_t bytes, at::Device device) {
-  const c10::cuda::CUDAStreamGuard guard(stream == nullptr || stream == cudaStreamLegacy
-                                             ? c10::cuda::getDefaultCUDAStream(device.index())
-                                             : c10::cuda::getStreamFromExternal(stream, device.index()));
+  const c10::cuda::CUDAStreamGuard guard(torch_stream(stream, device));
   return empty({static_cast<int64_t>(bytes < 16 ? 16 : bytes)}, at::kByte, device);
 }
 
@@ -296,11 +321,11 @@ PyObject *sample(PyObject *const *a) {
   const at::Tensor *status = optional_tensor(a[kStatus], "status");
   if (status && (!status->is_cuda() || !has_dtype(*status, at::kInt) || status->numel() < 1))
     value_error("status must be an int32 CUDA tensor");
-  const Output tok = output(a[kTok], "out_tok", true, {l.rows}, at::kInt, l.device);
-  const Output logp = output(a[kLogp], "out_logp", truth(a[kWantLogp]), {l.rows}, at::kFloat, l.device);
-  const Output ent = output(a[kEnt], "out_ent", truth(a[kWantEnt]), {l.rows}, at::kFloat, l.device);
-  const Output gap = output(a[kGap], "out_gap", truth(a[kWantGap]), {l.rows}, at::kFloat, l.device);
-  const cudaStream_t stream = stream_of(a[kStream]);
+  const CallStream stream(a[kStream], l.device);
+  const Output tok = output(a[kTok], "out_tok", true, {l.rows}, at::kInt, stream);
+  const Output logp = output(a[kLogp], "out_logp", truth(a[kWantLogp]), {l.rows}, at::kFloat, stream);
+  const Output ent = output(a[kEnt], "out_ent", truth(a[kWantEnt]), {l.rows}, at::kFloat, stream);
+  const Output gap = output(a[kGap], "out_gap", truth(a[kWantGap]), {l.rows}, at::kFloat, stream);
   // the blocked sampler asks for its full size; for the others the room for cut rows is enough (that of a training pass of no rows)
   const size_t need = sampler == E3_SAMPLER_BLOCK ? e3_workspace_bytes(E3_CALL_SAMPLE, l.rows, l.V, l.dt)
                                                   : e3_workspace_bytes(E3_CALL_TOKEN_LOGP_ENTROPY, 0, l.V, l.dt);
@@ -327,10 +352,10 @@ PyObject *token_logp_entropy(PyObject *const *a) {
     value_error("out_sum must be a contiguous float64 CUDA tensor with two entries");
   if (status && (!status->is_cuda() || !has_dtype(*status, at::kInt) || status->numel() < 1))
     value_error("status must be an int32 CUDA tensor");
-  const Output logp = output(a[kLogp], "out_logp", true, {l.rows}, at::kFloat, l.device);
-  const Output ent = output(a[kEnt], "out_ent", true, {l.rows}, at::kFloat, l.device);
-  const Output gap = output(a[kGap], "out_gap", truth(a[kWantGap]), {l.rows}, at::kFloat, l.device);
-  const cudaStream_t stream = stream_of(a[kStream]);
+  const CallStream stream(a[kStream], l.device);
+  const Output logp = output(a[kLogp], "out_logp", true, {l.rows}, at::kFloat, stream);
+  const Output ent = output(a[kEnt], "out_ent", true, {l.rows}, at::kFloat, stream);
+  const Output gap = output(a[kGap], "out_gap", truth(a[kWantGap]), {l.rows}, at::kFloat, stream);
   const Scratch ws = scratch(a[kWorkspace], e3_workspace_bytes(E3_CALL_TOKEN_LOGP_ENTROPY, l.rows, l.V, l.dt), l.device, stream);
   double *const s = pointer<double>(sum);
   check("e3_token_logp_entropy", launch([&] {
@@ -357,10 +382,10 @@ PyObject *token_logp_entropy_backward(PyObject *const *a) {
   if (!has_dtype(*t[kTargets], at::kInt) || !has_dtype(*t[kLogp], at::kFloat) || !has_dtype(*t[kEnt], at::kFloat))
     value_error("targets must be int32, logp and ent float32");
   const float tau = number(a[kTempScalar]);
-  const Output out = output(a[kOut], "out", true, {l.rows, l.V}, logits.scalar_type(), l.device);
+  const CallStream stream(a[kStream], l.device);
+  const Output out = output(a[kOut], "out", true, {l.rows, l.V}, logits.scalar_type(), stream);
   Logits o = out.object ? logits_of(required_tensor(a[kOut], "out")) : logits_of(out.made);
   if (o.dt != l.dt || o.rows != l.rows || o.V != l.V) value_error("out must have the shape and dtype of logits");
-  const cudaStream_t stream = stream_of(a[kStream]);
   check("e3_token_logp_entropy_backward", launch([&] {
           return e3_token_logp_entropy_backward(l.data, l.dt, l.rows, l.V, l.stride, pointer<int32_t>(t[kTargets]),
                                                 pointer<uint8_t>(t[kMask]), pointer<float>(t[kTemps]), tau, pointer<float>(t[kLogp]),
@@ -382,8 +407,8 @@ PyObject *masked_mean_entropy(PyObject *const *a) {
   const at::Tensor *mask = device_tensor(a[kMask], "mask");
   check_tokens(ent, mask);
   const int64_t n = ent.numel();
-  const Output out = output(a[kOut], "out", true, {2}, at::kDouble, ent.device());
-  const cudaStream_t stream = stream_of(a[kStream]);
+  const CallStream stream(a[kStream], ent.device());
+  const Output out = output(a[kOut], "out", true, {2}, at::kDouble, stream);
   const Scratch ws = scratch(a[kWorkspace], e3_workspace_bytes(E3_CALL_MASKED_MEAN_ENTROPY, n, 0, E3_F32), ent.device(), stream);
   double *const o = out.data<double>();
   check("e3_masked_mean_entropy", launch([&] {
@@ -400,8 +425,8 @@ PyObject *sequence_mean_entropy(PyObject *const *a) {
     value_error("ent must be a contiguous float32 tensor [n_seq, seq_len]");
   if (mask && (!has_dtype(*mask, at::kByte) || mask->numel() != ent.numel() || !mask->is_contiguous()))
     value_error("mask must be contiguous uint8 with one entry per token");
-  const Output out = output(a[kOut], "out", true, {2}, at::kDouble, ent.device());
-  const cudaStream_t stream = stream_of(a[kStream]);
+  const CallStream stream(a[kStream], ent.device());
+  const Output out = output(a[kOut], "out", true, {2}, at::kDouble, stream);
   const Scratch ws = scratch(a[kWorkspace], e3_workspace_bytes(E3_CALL_SEQUENCE_MEAN_ENTROPY, ent.size(0), 0, E3_F32), ent.device(), stream);
   double *const o = out.data<double>();
   check("e3_sequence_mean_entropy", launch([&] {
@@ -416,8 +441,8 @@ PyObject *masked_mean_entropy_static(PyObject *const *a) {
   const at::Tensor &ent = required_tensor(a[kEnt], "ent");
   const at::Tensor *mask = device_tensor(a[kMask], "mask");
   check_tokens(ent, mask);
-  const Output out = output(a[kOut], "out", true, {2}, at::kDouble, ent.device());
-  const cudaStream_t stream = stream_of(a[kStream]);
+  const CallStream stream(a[kStream], ent.device());
+  const Output out = output(a[kOut], "out", true, {2}, at::kDouble, stream);
   double *const o = out.data<double>();
   check("e3_masked_mean_entropy_static", launch([&] {
           return e3_masked_mean_entropy_static(pointer<float>(ent), pointer<uint8_t>(mask), ent.numel(), o, o + 1, stream);
@@ -434,13 +459,13 @@ PyObject *group_advantage(PyObject *const *a) {
   const float eps = number(a[kEps]);
   const int unbiased = truth(a[kUnbiased]) ? 1 : 0;
   const bool own_adv = a[kAdv] == Py_None, own_flags = a[kFlags] == Py_None && truth(a[kWantFlags]);
-  Output adv = output(a[kAdv], "out_adv", rewards.is_contiguous(), rewards.sizes(), at::kFloat, rewards.device());
+  const CallStream stream(a[kStream], rewards.device());
+  Output adv = output(a[kAdv], "out_adv", rewards.is_contiguous(), rewards.sizes(), at::kFloat, stream);
   if (!adv.any) {  // groups go by the order in memory: permuted rewards give advantages permuted alike
-    adv.made = at::empty_like(rewards);
+    adv.made = stream.make([&] { return at::empty_like(rewards); });
     adv.any = true;
   }
-  const Output flags = output(a[kFlags], "out_flags", own_flags, {ng < 0 ? 0 : ng}, at::kByte, rewards.device());
-  const cudaStream_t stream = stream_of(a[kStream]);
+  const Output flags = output(a[kFlags], "out_flags", own_flags, {ng < 0 ? 0 : ng}, at::kByte, stream);
   check("e3_group_advantage", launch([&] {
           if (own_adv && (own_flags || !flags.any))  // new tensors: what no group covers reads 0
             return e3::group_advantage_filled(pointer<float>(rewards), rewards.numel(), pointer<int64_t>(offsets), ng, eps, unbiased,
@@ -469,9 +494,9 @@ PyObject *grpo_objective(PyObject *const *a) {
   if (mask && (!has_dtype(*mask, at::kByte) || mask->numel() != n_seq * seq_len || !mask->is_contiguous()))
     value_error("mask must be contiguous uint8 with one entry per token");
   const float clip = number(a[kClip]);
-  const Output grad = output(a[kGrad], "out_g_logp", truth(a[kWantGrad]), {n_seq, seq_len}, at::kFloat, logp.device());
-  const Output out = output(a[kOut], "out", true, {2}, at::kDouble, logp.device());
-  const cudaStream_t stream = stream_of(a[kStream]);
+  const CallStream stream(a[kStream], logp.device());
+  const Output grad = output(a[kGrad], "out_g_logp", truth(a[kWantGrad]), {n_seq, seq_len}, at::kFloat, stream);
+  const Output out = output(a[kOut], "out", true, {2}, at::kDouble, stream);
   const Scratch ws = scratch(a[kWorkspace], e3_workspace_bytes(E3_CALL_GRPO_OBJECTIVE, n_seq, 0, E3_F32), logp.device(), stream);
   double *const o = out.data<double>();
   check("e3_grpo_objective", launch([&] {
@@ -505,11 +530,12 @@ const at::Tensor *checked(const OnDevice &on, const at::Tensor *t, const char *n
   }
   return t;
 }
-Output checked_output(const OnDevice &on, PyObject *given, const char *name, bool make, at::IntArrayRef size, at::ScalarType dtype) {
+Output checked_output(const OnDevice &on, PyObject *given, const char *name, bool make, at::IntArrayRef size, at::ScalarType dtype,
+                      const CallStream &stream) {
   int64_t n = 1;
   for (int64_t s : size) n *= s;
   checked(on, device_tensor(given, name), name, dtype, n);
-  return output(given, name, make, size, dtype, on.device);
+  return output(given, name, make, size, dtype, stream);
 }
 // A matrix with a contiguous last dimension.
 struct Matrix {
@@ -565,11 +591,11 @@ PyObject *verify_drafts(PyObject *const *a) {
     draft_temps = checked(on, device_tensor(a[kDraftTemps], "draft_temps"), "draft_temps", at::kFloat, n);
     draft_logp = checked(on, &required_tensor(a[kDraftLogp], "draft_logp"), "draft_logp", at::kFloat, n * k);
   }
-  const Output tok = checked_output(on, a[kTok], "out_tok", true, {n, k + 1}, at::kInt);
-  const Output kept = checked_output(on, a[kKept], "out_kept", true, {n}, at::kInt);
-  const Output logp = checked_output(on, a[kLogp], "out_logp", truth(a[kWantLogp]), {n, k + 1}, at::kFloat);
-  const Output ent = checked_output(on, a[kEnt], "out_ent", truth(a[kWantEnt]), {n, k + 1}, at::kFloat);
-  const cudaStream_t stream = stream_of(a[kStream]);
+  const CallStream stream(a[kStream], on.device);
+  const Output tok = checked_output(on, a[kTok], "out_tok", true, {n, k + 1}, at::kInt, stream);
+  const Output kept = checked_output(on, a[kKept], "out_kept", true, {n}, at::kInt, stream);
+  const Output logp = checked_output(on, a[kLogp], "out_logp", truth(a[kWantLogp]), {n, k + 1}, at::kFloat, stream);
+  const Output ent = checked_output(on, a[kEnt], "out_ent", truth(a[kWantEnt]), {n, k + 1}, at::kFloat, stream);
   const Scratch ws = checked_scratch(on, a[kWorkspace], e3_workspace_bytes(E3_CALL_VERIFY_DRAFTS, l.rows, l.V, l.dt), stream);
   check("e3_verify_drafts", launch([&] {
           return e3_verify_drafts(l.data, l.dt, n, k, l.V, l.stride, pointer<float>(temps), pointer<int32_t>(drafts), pointer<int32_t>(len),
@@ -588,6 +614,7 @@ PyObject *embed_tokens(PyObject *const *a) {
   const e3_dtype dt = dtype_of(table, "table");
   checked(on, &tok, "tok", at::kInt, tok.numel());
   const float scale = number(a[kScale]);
+  const CallStream stream(a[kStream], on.device);
   Output out;
   Matrix o = {};
   if (const at::Tensor *given = device_tensor(a[kOut], "out")) {
@@ -599,11 +626,10 @@ PyObject *embed_tokens(PyObject *const *a) {
   } else {
     c10::SmallVector<int64_t, 5> size(tok.sizes().begin(), tok.sizes().end());
     size.push_back(t.cols);
-    out = output(a[kOut], "out", true, size, table.scalar_type(), on.device);
+    out = output(a[kOut], "out", true, size, table.scalar_type(), stream);
     o.data = out.data<void>();
     o.stride = t.cols;
   }
-  const cudaStream_t stream = stream_of(a[kStream]);
   check("e3_embed_tokens", launch([&] {
           return e3_embed_tokens(pointer<int32_t>(tok), tok.numel(), t.data, dt, t.rows, t.cols, t.stride, scale, o.data, o.stride, stream);
         }));
@@ -625,12 +651,12 @@ PyObject *embed_tokens_backward(PyObject *const *a) {
   if (accumulate && !given) value_error("accumulate needs out");
   if (given && code >= 0 && !has_dtype(*given, type)) value_error("out is not of that dtype");
   if (!given && V < 1) check("e3_embed_tokens_backward", E3_ERR_INVALID_ARG);
-  const Output out = output(a[kOut], "out", true, {V, g.cols}, type, on.device);
+  const CallStream stream(a[kStream], on.device);
+  const Output out = output(a[kOut], "out", true, {V, g.cols}, type, stream);
   const at::Tensor &table = given ? *given : out.made;
   const Matrix o = matrix_of(on, table, "out");
   const e3_dtype table_dt = dtype_of(table, "out");
   if (o.rows != V || o.cols != g.cols) value_error("out must be [V, D]");
-  const cudaStream_t stream = stream_of(a[kStream]);
   const Scratch ws = checked_scratch(on, a[kWorkspace], e3_embed_workspace_bytes(g.rows, V, g.cols), stream);
   check("e3_embed_tokens_backward", launch([&] {
           return e3_embed_tokens_backward(pointer<int32_t>(tok), g.rows, g.data, dt, V, g.cols, g.stride, scale, o.data, table_dt, o.stride,
@@ -648,6 +674,7 @@ PyObject *quantize(PyObject *const *a) {
   const int64_t block_rows = static_cast<int64_t>(integer(a[kBlockRows]));
   if (block_rows != 1 && block_rows != E3_SCALE_BLOCK) value_error("block_rows must be 1 or 128");
   const int64_t nr = (m.rows + block_rows - 1) / block_rows, nc = (m.cols + E3_SCALE_BLOCK - 1) / E3_SCALE_BLOCK;
+  const CallStream stream(a[kStream], on.device);
   Output q;
   Matrix o = {};
   if (const at::Tensor *given = device_tensor(a[kQ], "out_q")) {
@@ -656,14 +683,13 @@ PyObject *quantize(PyObject *const *a) {
     q.object = a[kQ];
   } else {
     const int64_t padded = (m.cols + 15) / 16 * 16;
-    q.made = empty({m.rows, padded}, at::kFloat8_e4m3fn, on.device);
+    q.made = stream.empty({m.rows, padded}, at::kFloat8_e4m3fn);
     if (padded != m.cols) q.made = q.made.narrow(1, 0, m.cols);
     o.data = q.made.data_ptr();
     o.stride = padded;
   }
   q.any = true;
-  const Output scale = checked_output(on, a[kScale], "out_scale", true, {nr, nc}, at::kFloat);
-  const cudaStream_t stream = stream_of(a[kStream]);
+  const Output scale = checked_output(on, a[kScale], "out_scale", true, {nr, nc}, at::kFloat, stream);
   check("e3_quantize", launch([&] {
           return e3_quantize(m.data, dt, m.rows, m.cols, m.stride, static_cast<int32_t>(block_rows), static_cast<uint8_t *>(o.data), o.stride,
                              scale.data<float>(), nc, stream);
@@ -691,12 +717,12 @@ PyObject *project_vocab(PyObject *const *a) {
   const at::Tensor *given = device_tensor(a[kOut], "out"), *status = device_tensor(a[kStatus], "status");
   if (given && code >= 0 && !has_dtype(*given, code == E3_BF16 ? at::kBFloat16 : at::kFloat)) value_error("out is not of that dtype");
   checked(on, status, "status", at::kInt, 1);
-  const Output out = output(a[kOut], "out", true, {x.rows, w.rows}, code == E3_F32 ? at::kFloat : at::kBFloat16, on.device);
+  const CallStream stream(a[kStream], on.device);
+  const Output out = output(a[kOut], "out", true, {x.rows, w.rows}, code == E3_F32 ? at::kFloat : at::kBFloat16, stream);
   const at::Tensor &logits = given ? *given : out.made;
   const Matrix o = matrix_of(on, logits, "out");
   const e3_dtype dt = dtype_of(logits, "out");
   if (o.rows != x.rows || o.cols != w.rows) value_error("out must be [rows, V]");
-  const cudaStream_t stream = stream_of(a[kStream]);
   check("e3_project_vocab", launch([&] {
           return e3_project_vocab(static_cast<uint8_t *>(x.data), pointer<float>(xs), x.rows, x.stride, sx.stride, static_cast<uint8_t *>(w.data),
                                   pointer<float>(ws), w.rows, w.stride, sw.stride, x.cols, o.data, dt, o.stride, pointer<int32_t>(status), stream);
