@@ -716,7 +716,8 @@ PyObject *project_vocab(PyObject *const *a) {
   const int code = static_cast<int>(static_cast<int64_t>(integer(a[kDtype])));
   const at::Tensor *given = device_tensor(a[kOut], "out"), *status = device_tensor(a[kStatus], "status");
   if (given && code >= 0 && !has_dtype(*given, code == E3_BF16 ? at::kBFloat16 : at::kFloat)) value_error("out is not of that dtype");
-  checked(on, status, "status", at::kInt, 1);
+  if (status) on.same(status, "status");
+  if (status && (!has_dtype(*status, at::kInt) || status->numel() < 1)) value_error("status must be an int32 CUDA tensor");
   const CallStream stream(a[kStream], on.device);
   const Output out = output(a[kOut], "out", true, {x.rows, w.rows}, code == E3_F32 ? at::kFloat : at::kBFloat16, stream);
   const at::Tensor &logits = given ? *given : out.made;
