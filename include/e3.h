@@ -290,7 +290,8 @@ E3_API e3_status e3_quantize(const void *x, e3_dtype dt, int64_t rows, int64_t c
  * The vocabulary's projection in 8 bits, whose logits the row calls take: with the values and scales of e3_quantize (or any other fp32
  * scales of the same layout)
  *   logits[r, v] = sum_k x_scale[r, k] w_scale[v / E3_SCALE_BLOCK, k] sum_{i in block k of E3_SCALE_BLOCK columns} x[r, i] w[v, i].
- * The products of a block are added in 32 bits, the blocks in fp32, and the logits rounded once.  For rollouts: there is no backward pass.
+ * The products of a block are added in 32 bits, the blocks in fp32, and the logits rounded once.  A block's two scales are multiplied in fp32 first: where
+ * that product lies outside its range, so do the logits (infinite or NaN from 2^128 on, fewer digits below 2^-126).  For rollouts: there is no backward pass.
  *
  *   x, x_scale    device e4m3 bytes [rows, D], float [rows, ceil(D / E3_SCALE_BLOCK)]: the hidden states
  *   w, w_scale    device e4m3 bytes [V, D], float [ceil(V / E3_SCALE_BLOCK), ceil(D / E3_SCALE_BLOCK)]: the table
