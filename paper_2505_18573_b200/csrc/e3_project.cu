@@ -583,7 +583,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t piece = ring + kStages * kStageBytes + warp * kOutBytes;
     uint32_t n = 0;
     bool on = true;
-    // scales of four blocks ahead, the next tile's first ones too: the row's, and the table's for these entries (multiplied when they are needed, or
+    // scales of kAhead blocks ahead, the next tile's first ones too: the row's, and the table's for these entries (multiplied when they are needed, or
     // the loads would be waited for here)
     float next_x[kAhead], next_w[kAhead];
     const float *sx, *sw, *next_sx, *next_sw;
