@@ -100,3 +100,24 @@ def test_outputs_that_the_current_stream_still_reads(e3, name):
         fresh = [torch.full_like(want.view(torch.uint8), 7) for _ in range(3)]
     torch.cuda.synchronize()
     assert torch.equal(copy.view(torch.uint8), want.view(torch.uint8)) and len(fresh) == 3
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_a_stream_that_joins_a_capture(e3, name):
+    """Captured through a second stream that the capture forks to, replayed twice, its output dropped last."""
+    call, want, other = ready(e3, name)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        here = torch.cuda.current_stream()
+        other.wait_stream(here)
+        out = call(other)
+        here.wait_stream(other)
+        copy = out.clone()
+    for _ in range(2):
+        out.view(torch.uint8).zero_()
+        copy.view(torch.uint8).zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(copy.view(torch.uint8), want.view(torch.uint8))
+    del out, copy
+    assert torch.full((1000,), 3, device="cuda").eq(3).all()
