@@ -27,7 +27,8 @@
  *     the stream; they touch memory only after that work has completed.
  *   - The return value reports what the host can see (bad sizes, NULL
  *     pointers, launch failure).  Problems only the device can see (NaN or
- *     +inf logit, a row of -inf only, tau < 0 or not finite) mark that row:
+ *     +inf logit, a row of -inf only, tau < 0 or not finite, or so small (4.3e-39) that
+ *     log2(e) / tau is not finite in fp32) mark that row:
  *     token -1, log-prob, entropy and gap NaN.  Other rows are unaffected.
  *   - Every wait inside a kernel is bounded (two seconds).  If one ever runs out, the thread block
  *     concerned gives up: its unfinished rows read token -1 / NaN and bit E3_STATUS_TIMEOUT is OR-ed

@@ -1017,7 +1017,8 @@ __global__ void __launch_bounds__(kThreads, CTAS) draw_kernel(const __grid_const
   w.V = p.V; w.tau = tau; w.R = rec.R; w.lnZ = rec.lnZ; w.kind = rec.kind; w.d = rec.tok; w.y_d = rec.y; w.lnq = rec.lnq;
   if (w.kind == kDistribution) {
     w.y = p.draft_logits + (b * p.drafts + a) * p.draft_row_bytes;
-    w.beta_d = 1.0 / (double)tau_d; w.cd = __fdiv_rn(kLog2e, tau_d); w.nq = (float)(rec.lnq * (1.0 / kLn2));
+    w.beta_d = 1.0 / (double)tau_d; w.cd = fminf(__fdiv_rn(kLog2e, tau_d), 3.4e38f);  // (times 0 is 0: logits that tie)
+    w.nq = (float)(rec.lnq * (1.0 / kLn2));
   }
   const float2 *const sums = p.sums + r * p.blocks;
   // ---- scores under p: of the draw itself, or upper bounds (a loop of one copy: a CTA runs through most of this once, and waits for its instructions)

@@ -160,3 +160,22 @@ def test_a_draft_almost_like_the_target(e3, dtype, error):
     s.draft_logp = s.draft_logp + 1e-4
     s.uniforms[:, 0] = 1 - 1e-9
     s.check(e3)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tau", [1e-40, 1e-45, 4e-39, 1e-37])
+def test_drafts_at_temperatures_next_to_0(e3, dtype, tau):
+    """The draft's logits tie at three places, of a third each, however small its temperature: log2(e) / tau is beyond fp32 below 4.3e-39."""
+    n, V = 32, 5 * BLOCK
+    s = Batch(10, n, 1, V, dtype)
+    places = [5, 3 * BLOCK + 1, 4 * BLOCK]
+    z = torch.zeros((n, 2, V), device="cuda")
+    z[:, :, places[0]], z[:, :, places[1]], z[:, :, places[2]] = 6.5, 8.25, 7.25
+    s.logits = z.view(2 * n, V).to(dtype)
+    y = torch.full((n, V), -3.0, device="cuda")
+    y[:, places] = 1.5
+    s.draft_logits, s.draft_tok, s.temps = y.to(dtype), torch.full_like(s.draft_tok, places[0]), torch.ones_like(s.temps)
+    s.draft_temps, s.draft_logp = torch.full((n,), tau, device="cuda"), torch.full((n, 1), -math.log(3.0), device="cuda")
+    s.uniforms[:, 0] = 0.9
+    tok, kept, _, _ = s.check(e3)
+    assert not kept.any() and 0 < int((tok[:, 0] == places[1]).sum()) < n
